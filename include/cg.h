@@ -573,6 +573,115 @@ CG_API cg_status cg_breshare(const uint64_t *z_i, const uint8_t *key_self, const
                       uint64_t nonce, uint64_t first, uint64_t *out, size_t n, void *stream);
 
 /*
+ * Embedding tables on replicated pairs, rows chosen by PUBLIC ids (positions, segments, public
+ * tokens): linear in the shared values, hence local on each component (Sec. III-B, "Linear
+ * operations").  Private ids are a matrix product with their one-hot rows.
+ *
+ *   cg_share_embedding      : (za, zb)[j, :] = alpha * (ta, tb)[ids[j], :],  j < n
+ *   cg_share_embedding_grad : (da, db)[v, :] = alpha * sum over the j with ids[j] = v of (ga, gb)[j, :],
+ *                             v < V: written in full (accumulate = 0; rows that no id names become
+ *                             zero), or added to what da, db hold (accumulate = 1; rows that no id
+ *                             names are neither read nor written)
+ *
+ *   ta, tb, da, db : [V, D] row-major      za, zb, ga, gb : [n, D] row-major
+ *   ids            : n device integers, signed, of id_bytes = 4 or 8 bytes, aligned to their size.
+ *                    One outside [0, V) is padding: its row of z is zero (in every share, hence a
+ *                    share of zero), and it adds to no row of d.
+ *   alpha          : public ring element, e.g. the root of D as a fixed-point word (the result then
+ *                    carries its fractional bits as well); 1 for none
+ *
+ * The sums are exact mod 2^64: the same bits whatever the order.  V and D are >= 1 and below 2^31, n
+ * below 2^31 (CG_ERR_SHAPE, CG_ERR_UNSUPPORTED); id_bytes and accumulate as listed (CG_ERR_SHAPE).
+ * Outputs must not overlap the inputs, the ids or each other (CG_ERR_ALIAS).  n == 0: the lookup does
+ * nothing, the gradient without accumulate is zero.
+ */
+CG_API cg_status cg_share_embedding(const uint64_t *ta, const uint64_t *tb, const void *ids, int id_bytes,
+                             uint64_t alpha, uint64_t *za, uint64_t *zb, size_t n, size_t V, size_t D,
+                             void *stream);
+
+CG_API cg_status cg_share_embedding_grad(const uint64_t *ga, const uint64_t *gb, const void *ids, int id_bytes,
+                                  uint64_t alpha, uint64_t *da, uint64_t *db, size_t n, size_t V, size_t D,
+                                  int accumulate, void *stream);
+
+/*
+ * Norms of query and key heads with the position rotation, around the protocol that finds the
+ * inverse root (not a local step).  x holds `heads` heads of `dim` words per row, the queries' and
+ * the keys' next to each other so that one call takes both, read in place from a wider row
+ * (ld_x >= heads*dim words from a row to the next, e.g. the packed output of their projection).
+ *
+ *   cg_share_head_sq_sum      : z_i[t,h] = sum_d x_i x_i + x_{i+1} x_i + x_i x_{i+1}: the party's additive
+ *                               share of the head's sum of squares, [rows, heads]
+ *   cg_share_head_norm_rotate : u = three-term product of x[t,h,:] with the shared word r[t,h] (the
+ *                               inverse norm, [rows, heads]); z_i[t,h,:] = u turned by the public angles
+ *                               of position pos[t]: for pair p < rot/2 of the first `rot` elements, with
+ *                               c = cos[pos[t], p] and s = sin[pos[t], p],
+ *                                 (u1, u2) -> (u1 c - u2 s, u1 s + u2 c)
+ *                               and the elements from `rot` on times 2^frac_bits.
+ *   cg_share_head_norm_rotate_grad : from the gradient pair g of z, with v = g turned back (the same
+ *                               formula with -s) on both components: dx_i = three-term product of
+ *                               v and r, dr_i[t,h] = sum_d of the three-term products of x and v.
+ *
+ *   cos, sin : [positions, rot/2] public ring words with frac_bits fractional bits; pos: rows device
+ *              integers, signed, of pos_bytes = 4 or 8 bytes.  A position outside [0, positions) gives
+ *              a row of zeros (z, dx and dr).
+ *   interleaved : 0 pairs element p with p + rot/2, 1 pairs 2p with 2p + 1
+ *   rot      : even, 0 <= rot <= dim; 0 turns nothing, and cos, sin, pos may be NULL (a three-term
+ *              product with one shared word per head, e.g. the last step of the norm's gradient)
+ *   ld_g, ld_out : words from a row to the next of g, and of z or dx (>= heads*dim; what lies
+ *              between the rows is left alone).  r, dr and the sums are contiguous.
+ *
+ * Results are additive shares at the product's scale (x, r and the angles' bits together), not re-shared, not
+ * truncated.  CG_ERR_SHAPE for a dimension that does not fit the above, CG_ERR_UNSUPPORTED if
+ * rows*heads exceeds 2^31-1.  Outputs must not overlap inputs or each other, from the first word to
+ * the last (CG_ERR_ALIAS).  rows == 0 returns CG_OK.
+ */
+typedef struct {
+    int64_t rows, heads, dim, rot, ld_x, ld_g, ld_out, positions, pos_bytes, frac_bits, interleaved;
+} cg_head_desc;
+
+CG_API cg_status cg_share_head_sq_sum(const uint64_t *x_i, const uint64_t *x_ip1, uint64_t *z_i, int64_t rows,
+                               int64_t heads, int64_t dim, int64_t ld_x, void *stream);
+
+CG_API cg_status cg_share_head_norm_rotate(const uint64_t *x_i, const uint64_t *x_ip1, const uint64_t *r_i,
+                                    const uint64_t *r_ip1, const uint64_t *cos, const uint64_t *sin,
+                                    const void *pos, uint64_t *z_i, const cg_head_desc *desc, void *stream);
+
+CG_API cg_status cg_share_head_norm_rotate_grad(const uint64_t *g_i, const uint64_t *g_ip1, const uint64_t *x_i,
+                                         const uint64_t *x_ip1, const uint64_t *r_i, const uint64_t *r_ip1,
+                                         const uint64_t *cos, const uint64_t *sin, const void *pos,
+                                         uint64_t *dx_i, uint64_t *dr_i, const cg_head_desc *desc, void *stream);
+
+/*
+ * Gradient clipping over many tensors.  The lists are HOST arrays of `count` device pointers and
+ * sizes, read during the call; entries of size 0 are skipped, count may be 0.
+ *
+ *   cg_share_sq_norm : z_i = sum over all elements of all tensors of x_i x_i + x_{i+1} x_i + x_i x_{i+1}:
+ *                      the party's additive share (one word) of the squared global norm, with twice
+ *                      the gradients' fractional bits
+ *   cg_clip_factor   : the public factor once the three shares s0, s1, s2 (device words) have been opened
+ *                      to each other: with S = s0 + s1 + s2 read as unsigned and N = floor(sqrt(S))
+ *                      (the norm, at the gradients' scale; max_norm is a word of that scale, too),
+ *                        factor = 2^frac_bits                          if N <= max_norm
+ *                                 floor(max_norm * 2^frac_bits / N)    otherwise.
+ *                      In integers, so that the parties get the same word.  factor may be one of
+ *                      s0, s1, s2.  CG_ERR_SHAPE unless 0 <= frac_bits <= 62 and max_norm * 2^frac_bits
+ *                      < 2^64.  (Opening the norm tells it to the parties.  A program that must not
+ *                      keeps the factor shared and multiplies with cg_share_mul, period 1.)
+ *   cg_share_clip    : (za, zb)[k][j] = factor * (xa, xb)[k][j] for all tensors, factor a device word;
+ *                      the result carries the factor's bits as well, until the protocol's truncation.
+ *                      za[k] may equal xa[k], zb[k] may equal xb[k]; apart from that no output
+ *                      may overlap an input, another output of any entry, or the factor (CG_ERR_ALIAS).
+ */
+CG_API cg_status cg_share_sq_norm(const uint64_t *const *x_i, const uint64_t *const *x_ip1, const size_t *n,
+                           size_t count, uint64_t *z_i, void *stream);
+
+CG_API cg_status cg_clip_factor(const uint64_t *s0, const uint64_t *s1, const uint64_t *s2, uint64_t max_norm,
+                         int frac_bits, uint64_t *factor, void *stream);
+
+CG_API cg_status cg_share_clip(const uint64_t *const *xa, const uint64_t *const *xb, const uint64_t *factor,
+                        uint64_t *const *za, uint64_t *const *zb, const size_t *n, size_t count, void *stream);
+
+/*
  * out = s0 + s1 + s2 (mod 2^64), element-wise over n (Sec. III-B, "Secret
  * sharing").  Opens a replicated sharing (pass its three distinct shares) and
  * equally the three parties' additive outputs z_0, z_1, z_2 of

@@ -11,11 +11,13 @@ paper's definition out as plain loops.  The binary-share section further down
 (the adder circuits for the most significant bit, their gates and the bit-plane
 helpers) is numpy arithmetic of this module's own: XOR / AND / shifts on whole
 arrays, written gate by gate, and pinned by the plain integer sum of the shares
-in ``tests/test_oracle_msb.py``.
+in ``tests/test_oracle_msb.py``.  So is the section on embeddings, heads and
+gradient clipping at the end, pinned by ``tests/test_oracle_heads.py``.
 """
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import subprocess
 
@@ -576,3 +578,76 @@ def sum_pool2d(X, window, stride, pad=(0, 0)) -> np.ndarray:
     Z = np.empty((B, Ho, Wo, C), dtype=np.uint64)
     lib().oracle_sum_pool2d(_p(X), _p(Z), B, H, Wd, C, kh, kw, stride[0], stride[1], pad[0], pad[1])
     return Z
+
+
+# ---- embedding, heads, gradient clipping: the definitions on numpy's unsigned words ----
+def embedding(T, ids, alpha: int = 1) -> np.ndarray:
+    """alpha * T[ids], zeros where an id is outside the table."""
+    T, ids = _u(T), np.asarray(ids)
+    z = np.zeros(ids.shape + T.shape[1:], dtype=np.uint64)
+    for at in np.ndindex(*ids.shape):
+        if 0 <= ids[at] < T.shape[0]:
+            z[at] = T[ids[at]] * np.uint64(alpha % (1 << 64))
+    return z
+
+
+def embedding_grad(G, ids, V: int, alpha: int = 1, old=None) -> np.ndarray:
+    """old + alpha * (sum of G's rows over each id's tokens), token by token."""
+    G, ids = _u(G), np.asarray(ids).reshape(-1)
+    G = G.reshape(ids.size, -1) if ids.size else np.zeros((0, G.shape[-1]), np.uint64)
+    d = np.zeros((V, G.shape[1]), dtype=np.uint64) if old is None else _u(old).copy()
+    for j, v in enumerate(ids):
+        if 0 <= v < V:
+            d[v] += G[j] * np.uint64(alpha % (1 << 64))
+    return d
+
+
+def three_terms(x_i, x_ip1, y_i, y_ip1) -> np.ndarray:
+    return _u(x_i) * _u(y_i) + _u(x_ip1) * _u(y_i) + _u(x_i) * _u(y_ip1)
+
+
+def head_sq_sum(x_i, x_ip1) -> np.ndarray:
+    return three_terms(x_i, x_ip1, x_i, x_ip1).sum(-1, dtype=np.uint64)
+
+
+def rotate(U, cos, sin, pos, frac_bits: int, interleaved: bool, back: bool = False) -> np.ndarray:
+    """The heads U [rows, heads, dim] turned by the angles of their row's position (turned back: by minus the angles), zero where
+    the position is outside the tables; pair by pair."""
+    U = _u(U)
+    z = U << np.uint64(frac_bits)
+    if cos is None:
+        return z
+    half = cos.shape[1]
+    for t, at in enumerate(np.asarray(pos)):
+        if not 0 <= at < cos.shape[0]:
+            z[t] = 0
+            continue
+        for p in range(half):
+            d1, d2 = (2 * p, 2 * p + 1) if interleaved else (p, p + half)
+            c, s = _u(cos)[at, p], _u(sin)[at, p]
+            if back:
+                s = np.uint64((-int(s)) % (1 << 64))
+            z[t, :, d1] = U[t, :, d1] * c - U[t, :, d2] * s
+            z[t, :, d2] = U[t, :, d1] * s + U[t, :, d2] * c
+    return z
+
+
+def head_norm_rotate(x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=None, frac_bits: int = 0, interleaved: bool = False):
+    return rotate(three_terms(x_i, x_ip1, _u(r_i)[..., None], _u(r_ip1)[..., None]), cos, sin, pos, frac_bits, interleaved)
+
+
+def head_norm_rotate_grad(g_i, g_ip1, x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=None, frac_bits: int = 0,
+                          interleaved: bool = False):
+    v_i, v_ip1 = (rotate(g, cos, sin, pos, frac_bits, interleaved, back=True) for g in (g_i, g_ip1))
+    return (three_terms(v_i, v_ip1, _u(r_i)[..., None], _u(r_ip1)[..., None]),
+            three_terms(x_i, x_ip1, v_i, v_ip1).sum(-1, dtype=np.uint64))
+
+
+def sq_norm(pairs) -> int:
+    """The party's share of the squared norm over many (x_i, x_ip1)."""
+    return sum(int(three_terms(a, b, a, b).sum(dtype=np.uint64)) for a, b in pairs) % (1 << 64)
+
+
+def clip_factor(S: int, max_norm: int, frac_bits: int) -> int:
+    N = math.isqrt(S % (1 << 64))
+    return 1 << frac_bits if N <= max_norm else (max_norm << frac_bits) // N

@@ -27,6 +27,8 @@ EXPORTS = ("cg_status_string", "cg_version", "cg_share_matmul", "cg_share_conv2d
            "cg_bzero_share", "cg_breshare", "cg_share_bias_add", "cg_share_col_sum",
            "cg_bit_transpose64", "cg_bshare_carry_level", "cg_bits_unpack", "cg_bshare_csa", "cg_bshare_half_adder",
            "cg_share_matmul_acc", "cg_share_conv2d_acc", "cg_share_matmul_f64limb", "cg_share_matmul_static",
+           "cg_share_embedding", "cg_share_embedding_grad", "cg_share_head_sq_sum", "cg_share_head_norm_rotate",
+           "cg_share_head_norm_rotate_grad", "cg_share_sq_norm", "cg_clip_factor", "cg_share_clip",
            "cg_share_matmul_prefers_workspace", "cg_share_conv2d_prefers_workspace",
            "cg_share_matmul_prefers_digit_workspace", "cg_share_conv2d_prefers_digit_workspace",
            "cg_share_matmul_workspace_bytes", "cg_share_conv2d_workspace_bytes",
@@ -45,6 +47,12 @@ class PoolDesc(ctypes.Structure):
     """Mirror of cg_pool2d_desc."""
     _fields_ = [(n, ctypes.c_int64) for n in
                 ("B", "H", "W", "C", "kh", "kw", "stride_h", "stride_w", "pad_h", "pad_w")]
+
+
+class HeadDesc(ctypes.Structure):
+    """Mirror of cg_head_desc."""
+    _fields_ = [(n, ctypes.c_int64) for n in
+                ("rows", "heads", "dim", "rot", "ld_x", "ld_g", "ld_out", "positions", "pos_bytes", "frac_bits", "interleaved")]
 
 
 class CgError(RuntimeError):
@@ -109,6 +117,15 @@ def lib() -> ctypes.CDLL:
         L.cg_share_conv2d_dgrad_ws.argtypes = [vp] * 5 + [ctypes.POINTER(ConvDesc), vp, sz, vp]
         L.cg_share_conv2d_dgrad_workspace_bytes.argtypes = [ctypes.POINTER(ConvDesc)]
         L.cg_share_conv2d_wgrad.argtypes = [vp] * 5 + [ctypes.POINTER(ConvDesc), vp]
+        L.cg_share_embedding.argtypes = [vp] * 3 + [ctypes.c_int, u64, vp, vp, sz, sz, sz, vp]
+        L.cg_share_embedding_grad.argtypes = [vp] * 3 + [ctypes.c_int, u64, vp, vp, sz, sz, sz, ctypes.c_int, vp]
+        head = ctypes.POINTER(HeadDesc)
+        L.cg_share_head_sq_sum.argtypes = [vp] * 3 + [i64] * 4 + [vp]
+        L.cg_share_head_norm_rotate.argtypes = [vp] * 8 + [head, vp]
+        L.cg_share_head_norm_rotate_grad.argtypes = [vp] * 11 + [head, vp]
+        L.cg_share_sq_norm.argtypes = [vp] * 3 + [sz, vp, vp]
+        L.cg_clip_factor.argtypes = [vp] * 3 + [u64, ctypes.c_int, vp, vp]
+        L.cg_share_clip.argtypes = [vp] * 6 + [sz, vp]
         for name in EXPORTS[2:-SIZE_EXPORTS]:
             getattr(L, name).restype = ctypes.c_int
         for name in EXPORTS[-SIZE_EXPORTS:]:
@@ -148,6 +165,14 @@ def _stream(stream) -> int:
             return _raw_stream(_device())
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _current(*tensors) -> None:
+    """Calls launch on the current device: all their tensors have to live there."""
+    d = _device() if _device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+    for t in tensors:
+        if t.get_device() != d:
+            raise ValueError(f"tensors must live on the current GPU ({d}), got one on {t.device}")
 
 
 def _check(status: int, where: str) -> None:
@@ -616,6 +641,185 @@ def cg_share_col_sum(xa, xb, za=None, zb=None, stream=None):
     _check(lib().cg_share_col_sum(_ptr(xa) if rows else 0, _ptr(xb) if rows else 0, _ptr(za) if cols else 0,
                                   _ptr(zb) if cols else 0, rows, cols, _stream(stream)), "cg_share_col_sum")
     return za, zb
+
+
+def _index_ptr(t: torch.Tensor) -> Tuple[int, int]:
+    """Address and bytes per entry of a tensor of ids or positions."""
+    if t.dtype not in (torch.int64, torch.int32):
+        raise TypeError(f"ids and positions are torch.int64 or torch.int32, got {t.dtype}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("ids and positions must be contiguous and live on the GPU")
+    return t.data_ptr(), 8 if t.dtype == torch.int64 else 4
+
+
+def cg_share_embedding(ta, tb, ids, alpha: int = 1, za=None, zb=None, stream=None):
+    """(za, zb)[..., :] = alpha * (ta, tb)[ids[...], :]: rows of the table pair [V, D] by public ids (int64 or int32, any
+    shape), a row of zeros where an id is outside [0, V)."""
+    if ta.shape != tb.shape or ta.dim() != 2:
+        raise ValueError("the table must be a pair of [V, D] tensors")
+    V, D = ta.shape
+    shape = (*ids.shape, D)
+    za = torch.empty(shape, dtype=torch.int64, device=ta.device) if za is None else za
+    zb = torch.empty(shape, dtype=torch.int64, device=ta.device) if zb is None else zb
+    if tuple(za.shape) != shape or tuple(zb.shape) != shape:
+        raise ValueError("output shape does not match")
+    _current(ta, tb, ids, za, zb)
+    ip, width = _index_ptr(ids)
+    _check(lib().cg_share_embedding(_ptr(ta), _ptr(tb), ip, width, int(alpha) % (1 << 64), _ptr(za), _ptr(zb), ids.numel(), V, D,
+                                    _stream(stream)), "cg_share_embedding")
+    return za, zb
+
+
+def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=None, accumulate: bool = False, stream=None):
+    """(da, db) [V, D]: alpha times the sum of the rows of the gradient pair g [..., D] over each id's tokens; accumulate=True
+    adds that to what da, db hold and leaves the rows of other ids alone."""
+    if ga.shape != gb.shape or ga.dim() < 1 or ga.shape[:-1] != ids.shape:
+        raise ValueError("gradient shape does not match the ids")
+    D = ga.shape[-1]
+    if accumulate and (da is None or db is None):
+        raise ValueError("accumulate needs the tensors to add to")
+    da = torch.empty((V, D), dtype=torch.int64, device=ga.device) if da is None else da
+    db = torch.empty((V, D), dtype=torch.int64, device=ga.device) if db is None else db
+    if tuple(da.shape) != (V, D) or tuple(db.shape) != (V, D):
+        raise ValueError("output shape does not match")
+    _current(ga, gb, ids, da, db)
+    ip, width = _index_ptr(ids)
+    _check(lib().cg_share_embedding_grad(_ptr(ga), _ptr(gb), ip, width, int(alpha) % (1 << 64), _ptr(da), _ptr(db), ids.numel(), V, D,
+                                         int(bool(accumulate)), _stream(stream)), "cg_share_embedding_grad")
+    return da, db
+
+
+def _head_rows(t: torch.Tensor, shape=None) -> Tuple[int, int]:
+    """Address and words from a row to the next of a [rows, heads, dim] tensor whose rows are whole but may lie apart."""
+    if t.dtype != torch.int64:
+        raise TypeError(f"ring tensors are torch.int64 (uint64 bit patterns), got {t.dtype}")
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError("heads must be [rows, heads, dim] tensors of one shape")
+    rows, heads, dim = t.shape
+    step, head, one = t.stride()
+    if (dim > 1 and one != 1) or (heads > 1 and head != dim):
+        raise ValueError("the heads of a row must lie next to each other")
+    return t.data_ptr(), step if rows > 1 else heads * dim
+
+
+def _head_pair(a, b, shape=None) -> Tuple[int, int, int]:
+    (pa, ld), (pb, ld_b) = _head_rows(a, shape), _head_rows(b, a.shape)
+    if ld != ld_b:
+        raise ValueError("both components must have their rows equally far apart")
+    return pa, pb, ld
+
+
+def cg_share_head_sq_sum(x_i, x_ip1, z_i=None, stream=None) -> torch.Tensor:
+    """z_i [rows, heads]: the party's additive share of each head's sum of squares; x [rows, heads, dim], a slice of wider rows
+    (packed queries, keys and values) as it is."""
+    pa, pb, ld = _head_pair(x_i, x_ip1)
+    rows, heads, dim = x_i.shape
+    z_i = torch.empty((rows, heads), dtype=torch.int64, device=x_i.device) if z_i is None else z_i
+    if tuple(z_i.shape) != (rows, heads):
+        raise ValueError("output shape does not match")
+    _current(x_i, x_ip1, z_i)
+    _check(lib().cg_share_head_sq_sum(pa, pb, _ptr(z_i), rows, heads, dim, ld, _stream(stream)), "cg_share_head_sq_sum")
+    return z_i
+
+
+def _head_desc(x_i, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved):
+    """The descriptor, and the addresses of the shared norms, of the angles and of the positions."""
+    rows, heads, dim = x_i.shape
+    if tuple(r_i.shape) != (rows, heads) or r_ip1.shape != r_i.shape:
+        raise ValueError("the norms must be a pair of [rows, heads] tensors")
+    _current(x_i, r_i, r_ip1)
+    if cos is None and sin is None and pos is None:
+        return HeadDesc(rows, heads, dim, 0, ld_x, ld_g, ld_out, 0, 8, frac_bits, int(bool(interleaved))), (_ptr(r_i), _ptr(r_ip1), 0, 0, 0)
+    if cos is None or sin is None or pos is None or cos.dim() != 2 or sin.shape != cos.shape or tuple(pos.shape) != (rows,):
+        raise ValueError("angles are a pair of [positions, rot / 2] tensors, with a position for each row")
+    _current(cos, sin, pos)
+    pp, width = _index_ptr(pos)
+    d = HeadDesc(rows, heads, dim, 2 * cos.shape[1], ld_x, ld_g, ld_out, cos.shape[0], width, frac_bits, int(bool(interleaved)))
+    return d, (_ptr(r_i), _ptr(r_ip1), _ptr(cos), _ptr(sin), pp)
+
+
+def cg_share_head_norm_rotate(x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=None, frac_bits: int = 0, interleaved: bool = False,
+                              z_i=None, stream=None) -> torch.Tensor:
+    """z_i [rows, heads, dim]: three-term product of each head with its shared inverse norm r [rows, heads], the first
+    rot = 2 * cos.shape[1] elements turned by the public angles of the row's position, the others times 2^frac_bits.  Without
+    angles the product alone, times 2^frac_bits."""
+    pa, pb, ld_x = _head_pair(x_i, x_ip1)
+    z_i = torch.empty(x_i.shape, dtype=torch.int64, device=x_i.device) if z_i is None else z_i
+    pz, ld_out = _head_rows(z_i, x_i.shape)
+    _current(x_ip1, z_i)
+    d, rest = _head_desc(x_i, ld_x, 0, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved)
+    _check(lib().cg_share_head_norm_rotate(pa, pb, *rest, pz, ctypes.byref(d), _stream(stream)), "cg_share_head_norm_rotate")
+    return z_i
+
+
+def cg_share_head_norm_rotate_grad(g_i, g_ip1, x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=None, frac_bits: int = 0,
+                                   interleaved: bool = False, dx_i=None, dr_i=None, stream=None):
+    """(dx_i [rows, heads, dim], dr_i [rows, heads]): the party's additive shares of the gradients with respect to the heads and
+    to their inverse norms, from the gradient pair g of cg_share_head_norm_rotate's result."""
+    pa, pb, ld_x = _head_pair(x_i, x_ip1)
+    qa, qb, ld_g = _head_pair(g_i, g_ip1, x_i.shape)
+    rows, heads, _ = x_i.shape
+    dx_i = torch.empty(x_i.shape, dtype=torch.int64, device=x_i.device) if dx_i is None else dx_i
+    dr_i = torch.empty((rows, heads), dtype=torch.int64, device=x_i.device) if dr_i is None else dr_i
+    pd, ld_out = _head_rows(dx_i, x_i.shape)
+    if tuple(dr_i.shape) != (rows, heads):
+        raise ValueError("output shape does not match")
+    _current(x_ip1, g_i, g_ip1, dx_i, dr_i)
+    d, rest = _head_desc(x_i, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved)
+    _check(lib().cg_share_head_norm_rotate_grad(qa, qb, pa, pb, *rest, pd, _ptr(dr_i), ctypes.byref(d), _stream(stream)),
+           "cg_share_head_norm_rotate_grad")
+    return dx_i, dr_i
+
+
+class ShareList:
+    """The tensors of many replicated pairs (a program's gradients) with their addresses, read once: the calls over many tensors
+    take one, made when the tensors are.  It keeps the tensors; one that is given other memory (set_, resize_) needs a new list."""
+
+    def __init__(self, a: Sequence[torch.Tensor], b: Sequence[torch.Tensor]):
+        self.a, self.b = tuple(a), tuple(b)
+        if [t.shape for t in self.a] != [t.shape for t in self.b]:
+            raise ValueError("the components' shapes do not match")
+        if len({t.device for t in self.a + self.b}) > 1:
+            raise ValueError("the tensors must live on one GPU")
+        count = len(self.a)
+        self.count, self.shapes = count, [t.shape for t in self.a]
+        self.pa = (ctypes.c_void_p * count)(*[_ptr(t) for t in self.a])
+        self.pb = (ctypes.c_void_p * count)(*[_ptr(t) for t in self.b])
+        self.n = (ctypes.c_size_t * count)(*[t.numel() for t in self.a])
+
+
+def cg_share_sq_norm(x: ShareList, z_i=None, stream=None) -> torch.Tensor:
+    """z_i [1]: the party's additive share of the squared norm over all tensors of the list."""
+    if z_i is None:
+        z_i = torch.empty((1,), dtype=torch.int64, device=x.a[0].device if x.count else "cuda")
+    elif z_i.numel() != 1:
+        raise ValueError("output shape does not match")
+    _current(z_i, *x.a[:1])
+    _check(lib().cg_share_sq_norm(x.pa, x.pb, x.n, x.count, _ptr(z_i), _stream(stream)), "cg_share_sq_norm")
+    return z_i
+
+
+def cg_clip_factor(s0, s1, s2, max_norm: int, frac_bits: int, factor=None, stream=None) -> torch.Tensor:
+    """factor [1]: 2^frac_bits, or that times max_norm / norm rounded down where the norm, the root of the opened sum s0 + s1 + s2
+    of one word each, is larger; max_norm is a fixed-point word of the gradients' scale."""
+    factor = torch.empty((1,), dtype=torch.int64, device=s0.device) if factor is None else factor
+    if any(t.numel() != 1 for t in (s0, s1, s2, factor)):
+        raise ValueError("the shares of the squared norm and the factor are one word each")
+    if not 0 <= int(max_norm) < 1 << 64:
+        raise ValueError("max_norm is a non-negative word")
+    _current(s0, s1, s2, factor)
+    _check(lib().cg_clip_factor(_ptr(s0), _ptr(s1), _ptr(s2), int(max_norm), frac_bits, _ptr(factor), _stream(stream)), "cg_clip_factor")
+    return factor
+
+
+def cg_share_clip(x: ShareList, factor, out: Optional[ShareList] = None, stream=None) -> ShareList:
+    """out = factor * x over all tensors of both components, factor one word on the GPU; in place without `out`."""
+    out = x if out is None else out
+    if out.shapes != x.shapes or factor.numel() != 1:
+        raise ValueError("operand shapes do not match")
+    _current(factor, *x.a[:1], *out.a[:1])
+    _check(lib().cg_share_clip(x.pa, x.pb, _ptr(factor), out.pa, out.pb, x.n, x.count, _stream(stream)), "cg_share_clip")
+    return out
 
 
 def cg_bshare_xor(xa, xb, ya, yb, za=None, zb=None, stream=None):

@@ -7,11 +7,18 @@
 #include <mutex>
 
 #include "cg.h"
+#include "cg_check.h"
 #include "prf.h"
 #include "share_gemm.h"
 #include "share_gemm_rns.h"
 
 namespace {
+
+using cg::aligned;
+using cg::all_aligned16;
+using cg::bad_overlap;
+using cg::check_ptrs;
+using cg::overlap;
 
 typedef uint64_t u64;
 
@@ -19,19 +26,6 @@ const int64_t MAX_DIM = 0x7FFFFFFF;      // M, N as 32-bit ints in the kernel
 const int64_t MAX_ROW_WORDS = 1 << 20;   // K: MAX_TILE_ROWS rows of K words stay below 2^31 bytes
 const int64_t MAX_LONG_ROW_WORDS = (int64_t)1 << 30;   // K of the matrix products: slice indices stay 32-bit
 const int64_t MAX_VIEW_BYTES = 0x7FFFFFFF;
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-// do [a, a+na) and [b, b+nb) (bytes) intersect?
-bool overlap(const void* a, u64 na, const void* b, u64 nb) {
-    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
-    return pa < pb + nb && pb < pa + na;
-}
-
-// element-wise calls: identical pointers are fine (in place), partial overlap is not
-bool bad_overlap(const void* out, const void* in, u64 bytes) {
-    return out != in && overlap(out, bytes, in, bytes);
-}
 
 bool mul_overflows(int64_t a, int64_t b, int64_t* out) { return __builtin_mul_overflow(a, b, out); }
 
@@ -580,20 +574,6 @@ cg_status launch_ew(size_t n, bool vec, const F& f, void* stream) {
     return hipGetLastError() == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
 
-cg_status check_ptrs(const void* const* ptrs, int count) {
-    for (int i = 0; i < count; ++i)
-        if (!ptrs[i]) return CG_ERR_NULL;
-    for (int i = 0; i < count; ++i)
-        if (!aligned(ptrs[i], 8)) return CG_ERR_ALIGN;
-    return CG_OK;
-}
-
-bool all_aligned16(const void* const* ptrs, int count) {
-    for (int i = 0; i < count; ++i)
-        if (!aligned(ptrs[i], 16)) return false;
-    return true;
-}
-
 cg_status check_product_ptrs(const u64* x_i, const u64* x_ip1, const u64* y_i, const u64* y_ip1, u64* z_i,
                              u64 x_bytes, u64 y_bytes, u64 z_bytes) {
     const void* ptrs[5] = {x_i, x_ip1, y_i, y_ip1, z_i};
@@ -622,7 +602,7 @@ const char* cg_status_string(cg_status s) {
     return "unknown cg_status";
 }
 
-int cg_version(void) { return 100; }
+int cg_version(void) { return 200; }
 
 }  // extern "C"
 

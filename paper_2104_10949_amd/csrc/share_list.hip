@@ -1,0 +1,233 @@
+// Gradient clipping on replicated shares: the squared norm over many tensors, the public clip factor, the scaling.
+//
+// Sum of squares: with x = s_0 + s_1 + s_2 one party's three-term product of x with itself is
+// x_i x_i + x_{i+1} x_i + x_i x_{i+1} = x_i (x_i + 2 x_{i+1}), one ring product per element; its sum over all elements
+// of all tensors is one additive share of the squared norm.  Everything is exact mod 2^64 whatever the order.
+// 16 bytes are read per element and one word is written: bound by memory.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <stdlib.h>
+
+#include <algorithm>
+
+#include "cg.h"
+#include "cg_check.h"
+
+namespace {
+
+using cg::aligned;
+using cg::check_ptrs;
+
+typedef uint64_t u64;
+
+const int THREADS = 256;
+
+// Tensors of one launch, by value in the kernel's arguments (4 KB): no copy to the device, nothing to keep alive.
+const int NORM_MAX = 128, CLIP_MAX = 88;
+
+struct NormArgs {
+    const u64 *a[NORM_MAX], *b[NORM_MAX];
+    u64 n[NORM_MAX];
+    unsigned first[NORM_MAX];   // block with the tensor's first chunk
+    int count;
+};
+
+struct ClipArgs {
+    const u64 *a[CLIP_MAX], *b[CLIP_MAX];
+    u64 *za[CLIP_MAX], *zb[CLIP_MAX];
+    u64 n[CLIP_MAX];
+    unsigned first[CLIP_MAX];
+    int count;
+};
+
+// tensor that a block works on
+template <class Args>
+__device__ __forceinline__ int tensor_of(const Args& t, unsigned block) {
+    int lo = 0, hi = t.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.first[mid] <= block) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__global__ void set_word_kernel(u64* z, u64 v) { *z = v; }
+
+__global__ __launch_bounds__(THREADS) void sq_norm_kernel(NormArgs t, u64 chunk, u64* z) {
+    const int k = tensor_of(t, blockIdx.x);
+    const u64 begin = (u64)(blockIdx.x - t.first[k]) * chunk, end = begin + chunk < t.n[k] ? begin + chunk : t.n[k];
+    const u64 *a = t.a[k], *b = t.b[k];
+    u64 sum = 0;
+    for (u64 i = begin + threadIdx.x; i < end; i += THREADS) sum += a[i] * (a[i] + 2 * b[i]);
+    __shared__ u64 part[THREADS];
+    part[threadIdx.x] = sum;
+    __syncthreads();
+    for (int h = THREADS / 2; h > 0; h >>= 1) {
+        if ((int)threadIdx.x < h) part[threadIdx.x] += part[threadIdx.x + h];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) atomicAdd(reinterpret_cast<unsigned long long*>(z), (unsigned long long)part[0]);
+}
+
+__global__ __launch_bounds__(THREADS) void clip_kernel(ClipArgs t, u64 chunk, const u64* __restrict__ factor) {
+    const int k = tensor_of(t, blockIdx.x);
+    const u64 begin = (u64)(blockIdx.x - t.first[k]) * chunk, end = begin + chunk < t.n[k] ? begin + chunk : t.n[k];
+    const u64 c = *factor;
+    for (u64 i = begin + threadIdx.x; i < end; i += THREADS) {
+        const u64 a = t.a[k][i], b = t.b[k][i];
+        t.za[k][i] = a * c;
+        t.zb[k][i] = b * c;
+    }
+}
+
+// Largest r with r * r <= v: bit by bit, in integers, so that the three parties' factors are the same word.
+__device__ u64 floor_sqrt(u64 v) {
+    u64 r = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const u64 t = r | ((u64)1 << bit);
+        if (t * t <= v) r = t;
+    }
+    return r;
+}
+
+__global__ void clip_factor_kernel(const u64* s0, const u64* s1, const u64* s2, u64 max_norm, int frac_bits, u64* factor) {
+    const u64 norm = floor_sqrt(*s0 + *s1 + *s2);
+    *factor = norm <= max_norm ? (u64)1 << frac_bits : (max_norm << frac_bits) / norm;
+}
+
+// ---- host ----
+struct Range {
+    uintptr_t begin, end;
+    size_t entry;    // which tensor
+    int part;        // 0, 1: the components read; 2, 3: the components written
+    bool operator<(const Range& o) const { return begin < o.begin; }
+};
+
+// Every word that is written is written once and read by nobody else: outputs meet neither each other nor an input,
+// except an output equal to the input of its own position.
+cg_status check_written(const u64* const* xa, const u64* const* xb, u64* const* za, u64* const* zb, const size_t* n,
+                        size_t count) {
+    Range* r = static_cast<Range*>(malloc(4 * count * sizeof(Range)));
+    if (!r) return CG_ERR_DEVICE;
+    size_t m = 0;
+    for (size_t k = 0; k < count; ++k) {
+        if (n[k] == 0) continue;
+        const void* p[4] = {xa[k], xb[k], za[k], zb[k]};
+        for (int part = 0; part < 4; ++part) {
+            if (part < 2 && p[part] == p[part + 2]) continue;   // in place
+            const uintptr_t b = reinterpret_cast<uintptr_t>(p[part]);
+            r[m++] = {b, b + n[k] * 8, k, part};
+        }
+    }
+    std::sort(r, r + m);
+    uintptr_t read_end = 0, written_end = 0;
+    bool bad = false;
+    for (size_t i = 0; i < m && !bad; ++i) {
+        const bool written = r[i].part >= 2;
+        bad = r[i].begin < written_end || (written && r[i].begin < read_end);
+        uintptr_t& end = written ? written_end : read_end;
+        if (r[i].end > end) end = r[i].end;
+    }
+    free(r);
+    return bad ? CG_ERR_ALIAS : CG_OK;
+}
+
+cg_status check_list(const u64* const* const* lists, int parts, const size_t* n, size_t count, u64* total) {
+    *total = 0;
+    if (count == 0) return CG_OK;
+    if (!n) return CG_ERR_NULL;
+    for (int p = 0; p < parts; ++p)
+        if (!lists[p]) return CG_ERR_NULL;
+    for (size_t k = 0; k < count; ++k) {
+        if (n[k] == 0) continue;
+        for (int p = 0; p < parts; ++p)
+            if (!lists[p][k]) return CG_ERR_NULL;
+        for (int p = 0; p < parts; ++p)
+            if (!aligned(lists[p][k], 8)) return CG_ERR_ALIGN;
+        if (n[k] > (SIZE_MAX >> 4) || __builtin_add_overflow(*total, (u64)n[k], total) || *total > (SIZE_MAX >> 4)) return CG_ERR_SHAPE;
+    }
+    return CG_OK;
+}
+
+// Words of a block's chunk: about `blocks` blocks together, and no less than what keeps one busy.
+u64 chunk_words(u64 total, u64 blocks) {
+    const u64 least = 4096, c = (total / blocks + 1023) / 1024 * 1024;
+    return c < least ? least : c;
+}
+
+}  // namespace
+
+extern "C" {
+
+cg_status cg_share_sq_norm(const uint64_t* const* x_i, const uint64_t* const* x_ip1, const size_t* n, size_t count,
+                           uint64_t* z_i, void* stream) {
+    if (!z_i) return CG_ERR_NULL;
+    if (!aligned(z_i, 8)) return CG_ERR_ALIGN;
+    const u64* const* lists[2] = {x_i, x_ip1};
+    u64 total;
+    if (cg_status st = check_list(lists, 2, n, count, &total)) return st;
+    for (size_t k = 0; k < count; ++k)
+        if (n[k] > 0 && (cg::overlap(z_i, 8, x_i[k], n[k] * 8) || cg::overlap(z_i, 8, x_ip1[k], n[k] * 8))) return CG_ERR_ALIAS;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipLaunchKernelGGL(set_word_kernel, dim3(1), dim3(1), 0, s, z_i, (u64)0);
+    const u64 chunk = chunk_words(total, 2048);
+    for (size_t k = 0; k < count;) {
+        NormArgs t;
+        t.count = 0;
+        u64 blocks = 0;
+        for (; k < count && t.count < NORM_MAX; ++k) {
+            if (n[k] == 0) continue;
+            t.a[t.count] = x_i[k];
+            t.b[t.count] = x_ip1[k];
+            t.n[t.count] = n[k];
+            t.first[t.count++] = (unsigned)blocks;
+            blocks += (n[k] + chunk - 1) / chunk;
+        }
+        if (t.count > 0) hipLaunchKernelGGL(sq_norm_kernel, dim3((unsigned)blocks), dim3(THREADS), 0, s, t, chunk, z_i);
+    }
+    return hipGetLastError() == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+cg_status cg_clip_factor(const uint64_t* s0, const uint64_t* s1, const uint64_t* s2, uint64_t max_norm, int frac_bits,
+                         uint64_t* factor, void* stream) {
+    const void* ptrs[4] = {s0, s1, s2, factor};
+    if (cg_status st = check_ptrs(ptrs, 4)) return st;
+    if (frac_bits < 0 || frac_bits > 62 || max_norm > (~(u64)0 >> frac_bits)) return CG_ERR_SHAPE;
+    hipLaunchKernelGGL(clip_factor_kernel, dim3(1), dim3(1), 0, static_cast<hipStream_t>(stream), s0, s1, s2, max_norm,
+                       frac_bits, factor);
+    return hipGetLastError() == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+cg_status cg_share_clip(const uint64_t* const* xa, const uint64_t* const* xb, const uint64_t* factor,
+                        uint64_t* const* za, uint64_t* const* zb, const size_t* n, size_t count, void* stream) {
+    if (!factor) return CG_ERR_NULL;
+    if (!aligned(factor, 8)) return CG_ERR_ALIGN;
+    const u64* const* lists[4] = {xa, xb, const_cast<const u64* const*>(za), const_cast<const u64* const*>(zb)};
+    u64 total;
+    if (cg_status st = check_list(lists, 4, n, count, &total)) return st;
+    for (size_t k = 0; k < count; ++k)
+        if (n[k] > 0 && (cg::overlap(factor, 8, za[k], n[k] * 8) || cg::overlap(factor, 8, zb[k], n[k] * 8))) return CG_ERR_ALIAS;
+    if (total == 0) return CG_OK;
+    if (cg_status st = check_written(xa, xb, za, zb, n, count)) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const u64 chunk = chunk_words(total, 16384);
+    for (size_t k = 0; k < count;) {
+        ClipArgs t;
+        t.count = 0;
+        u64 blocks = 0;
+        for (; k < count && t.count < CLIP_MAX; ++k) {
+            if (n[k] == 0) continue;
+            t.a[t.count] = xa[k];
+            t.b[t.count] = xb[k];
+            t.za[t.count] = za[k];
+            t.zb[t.count] = zb[k];
+            t.n[t.count] = n[k];
+            t.first[t.count++] = (unsigned)blocks;
+            blocks += (n[k] + chunk - 1) / chunk;
+        }
+        if (t.count > 0) hipLaunchKernelGGL(clip_kernel, dim3((unsigned)blocks), dim3(THREADS), 0, s, t, chunk, factor);
+    }
+    return hipGetLastError() == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+}  // extern "C"

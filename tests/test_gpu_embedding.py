@@ -1,0 +1,230 @@
+"""Embedding lookup and its gradient on the GPU against the oracle: every bit of every row, at the sizes, ids and alignments where
+the kernels change their way of working, and nothing written beside the outputs."""
+import numpy as np
+import pytest
+
+from tests.gpu_util import first_mismatch, say
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def cg():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2104_10949_amd import binding
+    binding.lib()
+    return binding
+
+
+@pytest.fixture(scope="module")
+def ro():
+    from oracle import ring_oracle
+    return ring_oracle
+
+
+@pytest.fixture(scope="module")
+def wl():
+    from paper_2104_10949_amd import workloads
+    return workloads
+
+
+def draw_ids(kind, n, V, seed):
+    rng = np.random.default_rng(seed)
+    if kind == "one":                                    # every token the same
+        return np.full(n, V - 1, np.int64)
+    if kind == "padding":
+        return np.full(n, -1, np.int64)
+    if kind == "rank":                                   # frequencies as of words: the first id half of the time
+        return (np.exp(rng.random(n) * np.log(V + 1)) - 1).astype(np.int64).clip(0, V - 1)
+    if kind == "position":
+        return np.arange(n) % V
+    ids = rng.integers(0, V, n)
+    if kind == "mixed":                                  # padding of every kind among them
+        bad = rng.random(n) < 0.3
+        ids[bad] = rng.choice([-1, V, V + 7, -2 ** 31, 2 ** 31 - 1], bad.sum())
+    return ids
+
+
+def place(cg, a, words=0):
+    """The words of `a` on the GPU, `words` behind a 256-byte boundary."""
+    flat = torch.empty(a.size + words, dtype=torch.int64, device="cuda")
+    t = flat[words:].view(a.shape)
+    t.copy_(cg.to_device(a) if a.size else t)
+    return t
+
+
+GUARD = 0x5A5A5A5A5A5A5A5A
+
+
+class Guarded:
+    """An output with guard words on both sides of it."""
+
+    def __init__(self, shape, words=0, fill=None):
+        size = int(np.prod(shape))
+        self.flat = torch.full((size + 64 + words,), GUARD, dtype=torch.int64, device="cuda")
+        self.lo, self.size = 32 + words, size
+        self.t = self.flat[self.lo:self.lo + size].view(shape)
+        if fill is not None:
+            self.t.copy_(torch.from_numpy(fill.view(np.int64)))
+
+    def host(self):
+        flat = self.flat.cpu().numpy()
+        assert (flat[:self.lo] == GUARD).all() and (flat[self.lo + self.size:] == GUARD).all(), "written beside the output"
+        return flat[self.lo:self.lo + self.size].view(np.uint64).reshape(tuple(self.t.shape))
+
+
+LOOKUPS = [(1, 1, 1), (1, 10, 512), (2, 3, 2), (3, 2, 515), (65, 50, 7), (64, 50, 8), (257, 100, 64), (1000, 33, 130), (5, 9, 1024), (3, 4, 4098),
+           (33, 1000, 2049), (4097, 64, 16), (100, 300, 768)]
+
+
+@pytest.mark.parametrize("n,V,D", LOOKUPS)
+@pytest.mark.parametrize("dtype,words", [(torch.int64, 0), (torch.int32, 0), (torch.int32, 1)])
+def test_lookup(cg, ro, wl, n, V, D, dtype, words):
+    say(f"lookup n={n} V={V} D={D} {dtype} {words} words off")
+    ids, alpha = draw_ids("mixed", n, V, n + V), 0x123456789ABCDEF1
+    T = [wl.draw_ring((V, D), 100 + k) for k in range(2)]
+    z = [Guarded((n, D), words) for _ in range(2)]
+    dev = torch.from_numpy(ids).to("cuda").to(dtype)
+    cg.cg_share_embedding(place(cg, T[0], words), place(cg, T[1], words), dev, alpha, za=z[0].t, zb=z[1].t)
+    for t, out in zip(T, z):
+        want = ro.embedding(t, ids, alpha)
+        assert np.array_equal(out.host(), want), first_mismatch(out.host(), want)
+
+
+def test_lookup_of_a_batch_and_of_nothing(cg, ro, wl):
+    T = [wl.draw_ring((20, 24), 110 + k) for k in range(2)]
+    ids = draw_ids("uniform", 42, 20, 5).reshape(2, 3, 7)
+    z = cg.cg_share_embedding(*(cg.to_device(t) for t in T), torch.from_numpy(ids).cuda())
+    assert z[0].shape == (2, 3, 7, 24)
+    for t, out in zip(T, z):
+        assert np.array_equal(cg.to_host(out), ro.embedding(t, ids))
+    none = torch.empty((0, 4), dtype=torch.int64, device="cuda")
+    z = cg.cg_share_embedding(*(cg.to_device(t) for t in T), none)
+    assert z[0].shape == (0, 4, 24)
+
+
+def test_lookup_beyond_32_bit_offsets(cg):
+    """A table whose last rows lie behind 2^32 bytes, and whose words lie behind 2^29."""
+    V, D = (1 << 20) + 3, 520
+    say(f"lookup in a table of {V} x {D} words")
+    T = torch.arange(V, dtype=torch.int64, device="cuda")[:, None] * 1000003 + torch.arange(D, device="cuda")
+    ids = torch.tensor([V - 1, 0, V - 2, 1 << 20], device="cuda")
+    za, zb = cg.cg_share_embedding(T, T, ids, 3)
+    want = (ids[:, None] * 1000003 + torch.arange(D, device="cuda")) * 3
+    assert torch.equal(za, want) and torch.equal(zb, want)
+
+
+# (n, V, D): one token to many, rows shorter and longer than a wave's piece, tables smaller and larger than the batch
+GRADS = [(1, 1, 1), (1, 700, 512), (2, 5, 3), (63, 7, 16), (64, 64, 64), (65, 1000, 30), (500, 3, 515), (777, 1531, 130), (2048, 100, 258),
+         (4096, 300, 8), (4097, 40, 64), (5000, 5000, 20), (3000, 9, 1030), (9001, 2000, 33), (20000, 700, 34), (16384, 16384, 6), (40000, 50, 18)]
+
+
+@pytest.mark.parametrize("n,V,D", GRADS)
+@pytest.mark.parametrize("kind", ["rank", "mixed", "one", "position"])
+def test_gradient(cg, ro, wl, n, V, D, kind):
+    say(f"gradient n={n} V={V} D={D} {kind}")
+    ids, alpha, words = draw_ids(kind, n, V, n + D), 0xFEDCBA9876543210 + n, int(kind == "mixed")
+    G = [wl.draw_ring((n, D), 120 + k) for k in range(2)]
+    dev = torch.from_numpy(ids).to("cuda").to(torch.int32 if kind == "rank" else torch.int64)
+    g = [place(cg, t, words) for t in G]
+    d = [Guarded((V, D), words) for _ in range(2)]
+    cg.cg_share_embedding_grad(*g, dev, V, alpha, da=d[0].t, db=d[1].t)
+    want = [ro.embedding_grad(t, ids, V, alpha) for t in G]
+    for w, out in zip(want, d):
+        assert np.array_equal(out.host(), w), first_mismatch(out.host(), w)
+    cg.cg_share_embedding_grad(*g, dev, V, alpha, da=d[0].t, db=d[1].t, accumulate=True)     # and once more on top
+    for w, out in zip(want, d):
+        assert np.array_equal(out.host(), w + w), first_mismatch(out.host(), w + w)
+
+
+@pytest.mark.parametrize("n", [0, 40, 5000, 20000])
+def test_gradient_of_padding_alone(cg, wl, n):
+    say(f"gradient of {n} tokens of padding")
+    V, D = 31, 22
+    g = [cg.to_device(wl.draw_ring((n, D), 130 + k)) for k in range(2)]
+    ids = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    old = wl.draw_ring((V, D), 132)
+    d = [Guarded((V, D), fill=old) for _ in range(2)]
+    cg.cg_share_embedding_grad(*g, ids, V, 5, da=d[0].t, db=d[1].t, accumulate=True)
+    assert all(np.array_equal(t.host(), old) for t in d)
+    cg.cg_share_embedding_grad(*g, ids, V, 5, da=d[0].t, db=d[1].t)
+    assert all(not t.host().any() for t in d)
+
+
+@pytest.mark.parametrize("n", [300, 20000])
+def test_gradient_on_another_stream_and_of_changing_ids(cg, ro, wl, n):
+    """Calls one after the other on one stream with ids and gradients overwritten in between, each checked."""
+    say(f"gradient on a stream of its own, n={n}")
+    V, D = 150, 40
+    s = torch.cuda.Stream()
+    ids = torch.empty(n, dtype=torch.int64, device="cuda")
+    g = [torch.empty((n, D), dtype=torch.int64, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    results, wants = [], []
+    with torch.cuda.stream(s):
+        for k, kind in enumerate(("rank", "one", "mixed", "uniform")):
+            host = draw_ids(kind, n, V, k)
+            G = [wl.draw_ring((n, D), 140 + 2 * k + c) for c in range(2)]
+            ids.copy_(torch.from_numpy(host).cuda())
+            for t, h in zip(g, G):
+                t.copy_(cg.to_device(h))
+            results.append(cg.cg_share_embedding_grad(*g, ids, V, 7, stream=s if k % 2 else None))
+            wants.append([ro.embedding_grad(h, host, V, 7) for h in G])
+    s.synchronize()
+    for got, want in zip(results, wants):
+        for a, w in zip(got, want):
+            assert np.array_equal(cg.to_host(a), w), first_mismatch(cg.to_host(a), w)
+
+
+@pytest.mark.parametrize("n", [300, 20000])
+def test_gradient_in_two_graphs(cg, ro, wl, n):
+    """Two captured calls, replayed in turn with new inputs and the program's own work in between."""
+    say(f"gradient in two graphs, n={n}")
+    V, D = 90, 36
+    state, graphs = [], []
+    for k in range(2):
+        ids = torch.from_numpy(draw_ids("rank", n, V, k)).cuda()
+        g = [cg.to_device(wl.draw_ring((n, D), 160 + c)) for c in range(2)]
+        d = [torch.zeros((V, D), dtype=torch.int64, device="cuda") for _ in range(2)]
+        cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1])
+            cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1], accumulate=True)
+        state.append((ids, g, d))
+        graphs.append(graph)
+    for turn in range(4):
+        for k in range(2):
+            ids, g, d = state[k]
+            host = draw_ids(["rank", "one", "mixed", "uniform"][turn], n, V, 10 * turn + k)
+            G = [wl.draw_ring((n, D), 170 + 10 * turn + 2 * k + c) for c in range(2)]
+            ids.copy_(torch.from_numpy(host))
+            for t, h in zip(g, G):
+                t.copy_(cg.to_device(h))
+            for t in d:
+                t.fill_(turn)
+            graphs[k].replay()
+            _ = cg.cg_share_embedding_grad(*state[1 - k][1], state[1 - k][0], V)      # the program's own work
+            if turn % 2:
+                torch.cuda.synchronize()
+            for t, h in zip(d, G):
+                want = ro.embedding_grad(h, host, V, 6)
+                assert np.array_equal(cg.to_host(t), want), first_mismatch(cg.to_host(t), want)
+
+
+def test_gradient_of_many_words(cg):
+    """Gradients behind 2^32 bytes and a table of as many: rows of ones, so that every sum is a count."""
+    n, V, D = 1 << 16, (1 << 17) + 1, 8200
+    say(f"gradient n={n} V={V} D={D}")
+    g = torch.ones((n, D), dtype=torch.int64, device="cuda")
+    ids = torch.full((n,), V - 1, dtype=torch.int64, device="cuda")
+    ids[::2] = torch.arange(0, n, 2, device="cuda") * 2
+    da, db = cg.cg_share_embedding_grad(g, g, ids, V, 2)
+    count = torch.bincount(ids, minlength=V) * 2
+    for d in (da, db):
+        assert torch.equal(d[:, 0], count) and torch.equal(d[:, D - 1], count) and torch.equal(d[V - 1], count[V - 1].expand(D))
+        assert int(d.sum(0).ne(2 * n).sum()) == 0
