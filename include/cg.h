@@ -590,10 +590,17 @@ CG_API cg_status cg_breshare(const uint64_t *z_i, const uint8_t *key_self, const
  *   alpha          : public ring element, e.g. the root of D as a fixed-point word (the result then
  *                    carries its fractional bits as well); 1 for none
  *
- * The sums are exact mod 2^64: the same bits whatever the order.  V and D are >= 1 and below 2^31, n
- * below 2^31 (CG_ERR_SHAPE, CG_ERR_UNSUPPORTED); id_bytes and accumulate as listed (CG_ERR_SHAPE).
+ * The sums are exact mod 2^64: the same bits whatever the order.  V and D are >= 1 (CG_ERR_SHAPE), n
+ * and V below 2^31 and D at most 2^22 (CG_ERR_UNSUPPORTED); id_bytes and accumulate as listed (CG_ERR_SHAPE).
  * Outputs must not overlap the inputs, the ids or each other (CG_ERR_ALIAS).  n == 0: the lookup does
  * nothing, the gradient without accumulate is zero.
+ *
+ * The gradient groups the tokens by id in scratch memory (device memory, 16-byte aligned, not
+ * overlapping an operand: CG_ERR_ALIAS) of cg_share_embedding_grad_workspace_bytes(n, V, D) bytes, whose
+ * contents are undefined afterwards; calls that may overlap in time, captured ones among
+ * them, need one each.  With less, misaligned, or none (NULL) it adds every token's row to the table word by word:
+ * the same bits, slower.  The query returns 0 for sizes where scratch memory is of no use, and for
+ * invalid ones.
  */
 CG_API cg_status cg_share_embedding(const uint64_t *ta, const uint64_t *tb, const void *ids, int id_bytes,
                              uint64_t alpha, uint64_t *za, uint64_t *zb, size_t n, size_t V, size_t D,
@@ -601,7 +608,9 @@ CG_API cg_status cg_share_embedding(const uint64_t *ta, const uint64_t *tb, cons
 
 CG_API cg_status cg_share_embedding_grad(const uint64_t *ga, const uint64_t *gb, const void *ids, int id_bytes,
                                   uint64_t alpha, uint64_t *da, uint64_t *db, size_t n, size_t V, size_t D,
-                                  int accumulate, void *stream);
+                                  int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+CG_API size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D);
 
 /*
  * Norms of query and key heads with the position rotation, around the protocol that finds the

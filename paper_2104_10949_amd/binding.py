@@ -33,8 +33,8 @@ EXPORTS = ("cg_status_string", "cg_version", "cg_share_matmul", "cg_share_conv2d
            "cg_share_matmul_prefers_digit_workspace", "cg_share_conv2d_prefers_digit_workspace",
            "cg_share_matmul_workspace_bytes", "cg_share_conv2d_workspace_bytes",
            "cg_share_matmul_digit_workspace_bytes", "cg_share_conv2d_digit_workspace_bytes",
-           "cg_share_conv2d_dgrad_workspace_bytes")
-SIZE_EXPORTS = 5      # the last entries return size_t, the first two a string and an int, the rest cg_status
+           "cg_share_conv2d_dgrad_workspace_bytes", "cg_share_embedding_grad_workspace_bytes")
+SIZE_EXPORTS = 6      # the last entries return size_t, the first two a string and an int, the rest cg_status
 
 
 class ConvDesc(ctypes.Structure):
@@ -118,7 +118,8 @@ def lib() -> ctypes.CDLL:
         L.cg_share_conv2d_dgrad_workspace_bytes.argtypes = [ctypes.POINTER(ConvDesc)]
         L.cg_share_conv2d_wgrad.argtypes = [vp] * 5 + [ctypes.POINTER(ConvDesc), vp]
         L.cg_share_embedding.argtypes = [vp] * 3 + [ctypes.c_int, u64, vp, vp, sz, sz, sz, vp]
-        L.cg_share_embedding_grad.argtypes = [vp] * 3 + [ctypes.c_int, u64, vp, vp, sz, sz, sz, ctypes.c_int, vp]
+        L.cg_share_embedding_grad.argtypes = [vp] * 3 + [ctypes.c_int, u64, vp, vp, sz, sz, sz, ctypes.c_int, vp, sz, vp]
+        L.cg_share_embedding_grad_workspace_bytes.argtypes = [sz] * 3
         head = ctypes.POINTER(HeadDesc)
         L.cg_share_head_sq_sum.argtypes = [vp] * 3 + [i64] * 4 + [vp]
         L.cg_share_head_norm_rotate.argtypes = [vp] * 8 + [head, vp]
@@ -278,6 +279,7 @@ def _ws(workspace) -> Tuple[int, int]:
 
 SCRATCH_LIMIT = 4 << 30   # bytes: a call that would take more runs without
 SCRATCH_SPARE = 8         # ... and so does one that would leave less than this part of the card's memory free
+SCRATCH_SMALL = 1 << 20   # bytes: a call that takes no more does not ask how much is free (its outputs come from the same cache)
 
 
 def _scratch_fits(nbytes: int, device) -> bool:
@@ -309,7 +311,7 @@ def _scratch(nbytes: int, device, stream) -> Optional[torch.Tensor]:
     call asks for none, names a stream, even the current one (the allocator would not know its order), is being captured (the
     graph would keep the memory), or where memory is short."""
     if nbytes == 0 or nbytes > SCRATCH_LIMIT or stream is not None or device.index != torch.cuda.current_device() or \
-            torch.cuda.is_current_stream_capturing() or not _scratch_fits(nbytes, device):
+            torch.cuda.is_current_stream_capturing() or (nbytes > SCRATCH_SMALL and not _scratch_fits(nbytes, device)):
         return None
     mode = _exchange_capture_mode(HIP_STREAM_CAPTURE_MODE_RELAXED)
     if mode is None:
@@ -670,9 +672,11 @@ def cg_share_embedding(ta, tb, ids, alpha: int = 1, za=None, zb=None, stream=Non
     return za, zb
 
 
-def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=None, accumulate: bool = False, stream=None):
+def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=None, accumulate: bool = False,
+                            workspace=None, stream=None):
     """(da, db) [V, D]: alpha times the sum of the rows of the gradient pair g [..., D] over each id's tokens; accumulate=True
-    adds that to what da, db hold and leaves the rows of other ids alone."""
+    adds that to what da, db hold and leaves the rows of other ids alone.  Scratch memory (any contiguous GPU tensor of
+    cg_share_embedding_grad_workspace_bytes) comes from torch's allocator for the time of the call if none is given (see _scratch)."""
     if ga.shape != gb.shape or ga.dim() < 1 or ga.shape[:-1] != ids.shape:
         raise ValueError("gradient shape does not match the ids")
     D = ga.shape[-1]
@@ -684,9 +688,17 @@ def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=Non
         raise ValueError("output shape does not match")
     _current(ga, gb, ids, da, db)
     ip, width = _index_ptr(ids)
-    _check(lib().cg_share_embedding_grad(_ptr(ga), _ptr(gb), ip, width, int(alpha) % (1 << 64), _ptr(da), _ptr(db), ids.numel(), V, D,
-                                         int(bool(accumulate)), _stream(stream)), "cg_share_embedding_grad")
+    n = ids.numel()
+    if workspace is None:
+        workspace = _scratch(lib().cg_share_embedding_grad_workspace_bytes(n, V, D), ga.device, stream)
+    wp, wb = _ws(workspace)
+    _check(lib().cg_share_embedding_grad(_ptr(ga), _ptr(gb), ip, width, int(alpha) % (1 << 64), _ptr(da), _ptr(db), n, V, D,
+                                         int(bool(accumulate)), wp, wb, _stream(stream)), "cg_share_embedding_grad")
     return da, db
+
+
+def cg_share_embedding_grad_workspace_bytes(n: int, V: int, D: int) -> int:
+    return int(lib().cg_share_embedding_grad_workspace_bytes(n, V, D))
 
 
 def _head_rows(t: torch.Tensor, shape=None) -> Tuple[int, int]:

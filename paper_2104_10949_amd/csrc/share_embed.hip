@@ -49,24 +49,24 @@ __global__ __launch_bounds__(THREADS) void embed_kernel(const u64* __restrict__ 
                                                         u64* __restrict__ zb, u64 n, u64 V, u64 D, int lg) {
     typedef typename Words<W>::type T;
     const int lane = threadIdx.x & ((1 << lg) - 1);
-    const u64 j = ((u64)blockIdx.x * THREADS + threadIdx.x) >> lg;
-    if (j >= n) return;
-    const u64 units = D / W, id = (u64)(long long)ids[j];   // a negative id is beyond every V
-    const u64 c0 = ((u64)blockIdx.y * UNROLL << lg) + lane;
-    const T *sa = reinterpret_cast<const T*>(ta + id * D), *sb = reinterpret_cast<const T*>(tb + id * D);
-    T *oa = reinterpret_cast<T*>(za + j * D), *ob = reinterpret_cast<T*>(zb + j * D);
-    const bool there = id < V;
-    T a[UNROLL], b[UNROLL];
+    const u64 units = D / W, c0 = ((u64)blockIdx.y * UNROLL << lg) + lane;
+    for (u64 j = ((u64)blockIdx.x * THREADS + threadIdx.x) >> lg; j < n; j += (u64)gridDim.x * THREADS >> lg) {
+        const u64 id = (u64)(long long)ids[j];   // a negative id is beyond every V
+        const T *sa = reinterpret_cast<const T*>(ta + id * D), *sb = reinterpret_cast<const T*>(tb + id * D);
+        T *oa = reinterpret_cast<T*>(za + j * D), *ob = reinterpret_cast<T*>(zb + j * D);
+        const bool there = id < V;
+        T a[UNROLL], b[UNROLL];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const u64 c = c0 + ((u64)u << lg);
-        a[u] = b[u] = T(0);
-        if (there && c < units) { a[u] = sa[c]; b[u] = sb[c]; }
-    }
+        for (int u = 0; u < UNROLL; ++u) {
+            const u64 c = c0 + ((u64)u << lg);
+            a[u] = b[u] = T(0);
+            if (there && c < units) { a[u] = sa[c]; b[u] = sb[c]; }
+        }
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const u64 c = c0 + ((u64)u << lg);
-        if (c < units) { oa[c] = a[u] * alpha; ob[c] = b[u] * alpha; }
+        for (int u = 0; u < UNROLL; ++u) {
+            const u64 c = c0 + ((u64)u << lg);
+            if (c < units) { __builtin_nontemporal_store(a[u] * alpha, oa + c); __builtin_nontemporal_store(b[u] * alpha, ob + c); }
+        }
     }
 }
 
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(THREADS) void clear_kernel(u64* a, u64* b, u64 n) {
     }
 }
 
-// Gradient: every token's row is added to its row of the table's gradient, word by word.
+// Gradient without scratch memory, many tokens: every token's row is added to its row of the table's gradient, word by word.
 template <class Id>
 __global__ __launch_bounds__(THREADS) void embed_grad_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
                                                              const Id* __restrict__ ids, u64 alpha, u64* da, u64* db,
@@ -91,14 +91,334 @@ __global__ __launch_bounds__(THREADS) void embed_grad_kernel(const u64* __restri
     }
 }
 
+// ---- gradient with scratch memory: tokens grouped by id, every row of the gradient written once ----
+// The sums do not depend on the order, so grouping is all the sorting there has to be: a count per row, a place in one
+// list for each row's tokens (handed out by a cursor, in whatever order), the list.  Then one group of lanes per row and
+// piece adds up the row's tokens and writes the row.  Rows of more than `most` tokens are cut into items of that many, which
+// are added to the row atomically: a frequent token must not keep one wave busy to the end.
+
+struct Item {
+    unsigned row, first, count, whole;   // whole: all of the row's tokens
+};
+
+struct Grouped {   // in the scratch memory
+    unsigned long long* cursor;   // tokens placed so far, and items in the upper half; starts at zero as the counts do
+    unsigned *count, *offset, *rank, *list;
+    Item* items;
+    u64 items_max, bytes;
+    unsigned most;      // tokens of an item, at most 64
+    bool one_block;     // the tokens are few enough for one block's LDS: no counts, offsets and ranks in memory
+};
+
+const int GROUP_THREADS = 1024, GROUP_TOKENS = 4;   // of a block that groups, and of each of its threads
+const int TABLE = 2 * GROUP_THREADS * GROUP_TOKENS; // places of its hash table: at most half full
+const unsigned EMPTY = ~0u;                         // no row: V < 2^31
+
+Grouped grouped_layout(char* p, u64 n, u64 V) {
+    Grouped g = {};
+    // a wave takes about a microsecond for four tokens: items short enough not to outlast a small call, and in a large one
+    // few enough atomics
+    g.most = n < 8 * 256 ? 8 : n < 64 * 256 ? (unsigned)(n / 256) : 64;
+    g.one_block = n <= GROUP_THREADS * GROUP_TOKENS;
+    g.items_max = (n < V ? n : V) + 2 * n / g.most;   // rows with tokens; of those with c > most, ceil(c / most) items each
+    u64 at = 0;
+    const auto take = [&](u64 bytes) { char* q = p + at; at += (bytes + 255) / 256 * 256; return q; };
+    g.cursor = reinterpret_cast<unsigned long long*>(take(8 + (g.one_block ? 0 : V * 4)));
+    g.count = reinterpret_cast<unsigned*>(g.cursor + 1);
+    if (!g.one_block) {
+        g.offset = reinterpret_cast<unsigned*>(take(V * 4));
+        g.rank = reinterpret_cast<unsigned*>(take(n * 4));
+    }
+    g.list = reinterpret_cast<unsigned*>(take(n * 4));
+    g.items = reinterpret_cast<Item*>(take(g.items_max * sizeof(Item)));
+    g.bytes = at;
+    return g;
+}
+
+__global__ __launch_bounds__(THREADS) void group_clear_kernel(unsigned* a, u64 n) {
+    for (u64 i = (u64)blockIdx.x * THREADS + threadIdx.x; i < n; i += (u64)gridDim.x * THREADS) a[i] = 0;
+}
+
+// Counts a block's tokens, those of j0 + k * GROUP_THREADS, in a hash table in LDS: slot[k] is the place of token k's id
+// (EMPTY for padding), rank[k] how many of the block's tokens of that id came before it.
+template <class Id>
+__device__ __forceinline__ void count_in_table(const Id* __restrict__ ids, u64 n, u64 V, u64 j0, unsigned* key, unsigned* count,
+                                               unsigned (&slot)[GROUP_TOKENS], unsigned (&rank)[GROUP_TOKENS]) {
+    u64 id[GROUP_TOKENS];
+#pragma unroll
+    for (int k = 0; k < GROUP_TOKENS; ++k) {
+        const u64 j = j0 + (u64)k * GROUP_THREADS;
+        id[k] = j < n ? (u64)(long long)ids[j] : ~(u64)0;
+    }
+    for (int i = threadIdx.x; i < TABLE; i += GROUP_THREADS) { key[i] = EMPTY; count[i] = 0; }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < GROUP_TOKENS; ++k) {
+        slot[k] = EMPTY;
+        if (id[k] >= V) continue;
+        unsigned at = ((unsigned)id[k] * 2654435769u) >> 19;   // 13 bits
+        for (;; at = (at + 1) & (TABLE - 1)) {                 // ends: there are fewer ids in the block than places
+            const unsigned was = atomicCAS(&key[at], EMPTY, (unsigned)id[k]);
+            if (was == EMPTY || was == (unsigned)id[k]) break;
+        }
+        slot[k] = at;
+        rank[k] = atomicAdd(&count[at], 1u);
+    }
+    __syncthreads();
+}
+static_assert(TABLE == 1 << 13, "the hash takes the upper 13 bits");
+
+// Sum over the threads before this one, and over all of them.  Every thread of the block calls it.
+__device__ __forceinline__ unsigned long long block_scan(unsigned long long own, unsigned long long* wave_sum, unsigned long long* all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    unsigned long long up_to = own;
+    for (int h = 1; h < 64; h <<= 1) {
+        const unsigned long long o = __shfl_up(up_to, h);
+        if (lane >= h) up_to += o;
+    }
+    if (lane == 63) wave_sum[wave] = up_to;
+    __syncthreads();
+    unsigned long long before = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < GROUP_THREADS / 64; ++w) {
+        const unsigned long long s = wave_sum[w];
+        if (w < wave) before += s;
+        sum += s;
+    }
+    *all = sum;
+    return before + up_to - own;
+}
+
+// Tokens in the lower half, items in the upper half of a row of c tokens.
+__device__ __forceinline__ unsigned long long tokens_and_items(unsigned c, unsigned most) {
+    return ((unsigned long long)((c + most - 1) / most) << 32) | c;
+}
+
+__device__ __forceinline__ void write_items(Item* items, unsigned row, unsigned first, unsigned c, unsigned most) {
+    const unsigned m = (c + most - 1) / most;
+    for (unsigned k = 0; k < m; ++k) items[k] = {row, first + k * most, k + 1 < m ? most : c - k * most, m == 1};
+}
+
+// Few tokens: the first block groups them all, while the others clear the gradient (no block is one that clears if it
+// is added to).  The rows with tokens are cleared, too: they are few where the table is large.
+template <class Id>
+__global__ __launch_bounds__(GROUP_THREADS) void group_few_kernel(const Id* __restrict__ ids, u64 n, u64 V, Grouped g,
+                                                                  u64* da, u64* db, u64 words, bool pairs) {
+    if (blockIdx.x > 0) {
+        const u64 step = (u64)(gridDim.x - 1) * GROUP_THREADS, i0 = (u64)(blockIdx.x - 1) * GROUP_THREADS + threadIdx.x;
+        if (pairs)
+            for (u64 i = i0; i < words / 2; i += step) {
+                __builtin_nontemporal_store(ull2(0), reinterpret_cast<ull2*>(da) + i);
+                __builtin_nontemporal_store(ull2(0), reinterpret_cast<ull2*>(db) + i);
+            }
+        else
+            for (u64 i = i0; i < words; i += step) {
+                __builtin_nontemporal_store((u64)0, da + i);
+                __builtin_nontemporal_store((u64)0, db + i);
+            }
+        return;
+    }
+    __shared__ unsigned key[TABLE], count[TABLE];
+    __shared__ unsigned long long wave_sum[GROUP_THREADS / 64];
+    unsigned slot[GROUP_TOKENS], rank[GROUP_TOKENS];
+    count_in_table(ids, n, V, threadIdx.x, key, count, slot, rank);
+    const int PLACES = TABLE / GROUP_THREADS;
+    const int p0 = threadIdx.x * PLACES;
+    unsigned c[PLACES];
+    unsigned long long own = 0, all;
+#pragma unroll
+    for (int k = 0; k < PLACES; ++k) {
+        c[k] = count[p0 + k];
+        own += tokens_and_items(c[k], g.most);
+    }
+    unsigned long long at = block_scan(own, wave_sum, &all);
+#pragma unroll
+    for (int k = 0; k < PLACES; ++k) {
+        write_items(g.items + (at >> 32), key[p0 + k], (unsigned)at, c[k], g.most);
+        count[p0 + k] = (unsigned)at;
+        at += tokens_and_items(c[k], g.most);
+    }
+    if (threadIdx.x == 0) *g.cursor = all;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < GROUP_TOKENS; ++k)
+        if (slot[k] != EMPTY) g.list[count[slot[k]] + rank[k]] = threadIdx.x + k * GROUP_THREADS;
+}
+
+// rank[j] = how many tokens of the same id came before.  A block adds one number per id to the row's count: atomics of
+// thousands of tokens on one word of memory wait for each other (65536 tokens, 7 % of them the same: 76 us without the
+// table, 10 with it).
+template <class Id>
+__global__ __launch_bounds__(GROUP_THREADS) void group_count_kernel(const Id* __restrict__ ids, u64 n, u64 V, Grouped g) {
+    __shared__ unsigned key[TABLE], count[TABLE];
+    const u64 j0 = (u64)blockIdx.x * (GROUP_THREADS * GROUP_TOKENS) + threadIdx.x;
+    unsigned slot[GROUP_TOKENS], rank[GROUP_TOKENS];
+    count_in_table(ids, n, V, j0, key, count, slot, rank);
+    for (int i = threadIdx.x; i < TABLE; i += GROUP_THREADS)
+        if (key[i] != EMPTY) count[i] = atomicAdd(g.count + key[i], count[i]);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < GROUP_TOKENS; ++k)
+        if (slot[k] != EMPTY) g.rank[j0 + (u64)k * GROUP_THREADS] = count[slot[k]] + rank[k];
+}
+
+__global__ __launch_bounds__(GROUP_THREADS) void group_offset_kernel(u64 V, Grouped g) {
+    __shared__ unsigned long long wave_sum[GROUP_THREADS / 64], base;
+    const u64 v = (u64)blockIdx.x * GROUP_THREADS + threadIdx.x;
+    const unsigned c = v < V ? g.count[v] : 0;
+    unsigned long long all, at = block_scan(tokens_and_items(c, g.most), wave_sum, &all);
+    if (threadIdx.x == 0) base = all ? atomicAdd(g.cursor, all) : 0;
+    __syncthreads();
+    at += base;
+    if (v < V) g.offset[v] = (unsigned)at;
+    write_items(g.items + (at >> 32), (unsigned)v, (unsigned)at, c, g.most);
+}
+
+// The first token_blocks blocks fill the list; the others clear the rows that items will be added to.
+template <class Id>
+__global__ __launch_bounds__(THREADS) void group_list_kernel(const Id* __restrict__ ids, u64 n, u64 V, u64 D, Grouped g,
+                                                             unsigned token_blocks, u64* da, u64* db) {
+    if (blockIdx.x < token_blocks) {
+        const u64 j = (u64)blockIdx.x * THREADS + threadIdx.x;
+        if (j >= n) return;
+        const u64 id = (u64)(long long)ids[j];
+        if (id < V) g.list[g.offset[id] + g.rank[j]] = (unsigned)j;
+        return;
+    }
+    const unsigned used = (unsigned)(*g.cursor >> 32);
+    for (unsigned k = blockIdx.x - token_blocks; k < used; k += gridDim.x - token_blocks) {
+        const Item it = g.items[k];
+        if (it.whole || it.first != g.offset[it.row]) continue;   // the first item of a row that has several
+        for (u64 c = threadIdx.x; c < D; c += THREADS) {
+            da[it.row * D + c] = 0;
+            db[it.row * D + c] = 0;
+        }
+    }
+}
+
+// Sum of the pieces of the rows list[0 .. count), loads of four rows under way at a time.  Lanes behind the row's end
+// read its last words and write nothing.
+template <int W>
+struct RowSum {
+    typedef typename Words<W>::type T;
+    static const int U = W == 2 ? 2 : 4;   // accesses per component and lane: 256 words a piece of a whole wave
+    static const int R = W == 2 ? 4 : 2;
+    T a[U], b[U];
+
+    template <int N>
+    __device__ __forceinline__ void add(const u64* __restrict__ ga, const u64* __restrict__ gb, const unsigned (&row)[N],
+                                        u64 D, const u64 (&c)[U]) {
+        T x[N][U], y[N][U];
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            const T *pa = reinterpret_cast<const T*>(ga + row[r] * D), *pb = reinterpret_cast<const T*>(gb + row[r] * D);
+#pragma unroll
+            for (int u = 0; u < U; ++u) { x[r][u] = __builtin_nontemporal_load(pa + c[u]); y[r][u] = __builtin_nontemporal_load(pb + c[u]); }
+        }
+#pragma unroll
+        for (int r = 0; r < N; ++r)
+#pragma unroll
+            for (int u = 0; u < U; ++u) { a[u] += x[r][u]; b[u] += y[r][u]; }
+    }
+
+    // WAVE: the whole wave works on one row: its tokens are uniform and the addresses scalar (count <= 64)
+    template <bool WAVE>
+    __device__ __forceinline__ void gather(const u64* __restrict__ ga, const u64* __restrict__ gb,
+                                           const unsigned* __restrict__ list, unsigned count, u64 D, const u64 (&c)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) a[u] = b[u] = T(0);
+        unsigned mine = 0;
+        const int lane = threadIdx.x & 63;
+        if (WAVE && lane < (int)count) mine = list[lane];
+        unsigned i = 0;
+        for (; i + R <= count; i += R) {
+            unsigned row[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) row[r] = WAVE ? __builtin_amdgcn_readlane(mine, i + r) : list[i + r];
+            add(ga, gb, row, D, c);
+        }
+        for (; i < count; ++i) {
+            const unsigned row[1] = {WAVE ? (unsigned)__builtin_amdgcn_readlane(mine, i) : list[i]};
+            add(ga, gb, row, D, c);
+        }
+    }
+};
+
+__device__ __forceinline__ void add_atomically(u64* p, u64 v) {
+    atomicAdd(reinterpret_cast<unsigned long long*>(p), (unsigned long long)v);
+}
+__device__ __forceinline__ void add_atomically(ull2* p, ull2 v) {
+    add_atomically(reinterpret_cast<u64*>(p), v.x);
+    add_atomically(reinterpret_cast<u64*>(p) + 1, v.y);
+}
+
+const int FILL_ACCESSES = 8;   // accesses per lane and component of a wave that clears: 8 KB in a row
+
+// The items, by blocks below item_blocks, the pieces of a row next to each other so that its memory is read in one go; the
+// other blocks clear the rows without tokens, in the order of the addresses.
+template <int W, bool WAVE>
+__global__ __launch_bounds__(THREADS) void group_sum_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb, u64 alpha,
+                                                            u64* da, u64* db, u64 V, u64 D, int accumulate, int lg,
+                                                            unsigned pieces, unsigned item_blocks, Grouped g) {
+    typedef typename Words<W>::type T;
+    const int U = RowSum<W>::U;
+    const unsigned units = (unsigned)(D / W);
+    if (blockIdx.x >= item_blocks) {
+        const u64 all = V * units, chunk = FILL_ACCESSES * 64;
+        const u64 step = (u64)(gridDim.x - item_blocks) * (THREADS / 64) * chunk;
+        T *pa = reinterpret_cast<T*>(da), *pb = reinterpret_cast<T*>(db);
+        for (u64 i0 = ((u64)(blockIdx.x - item_blocks) * (THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * chunk; i0 < all;
+             i0 += step) {
+            const u64 row0 = i0 / units;
+            const unsigned c0 = (unsigned)(i0 - row0 * units);
+#pragma unroll
+            for (int k = 0; k < FILL_ACCESSES; ++k) {
+                const unsigned off = k * 64 + (threadIdx.x & 63);
+                if (i0 + off < all && g.count[row0 + (c0 + off) / units] == 0) {
+                    __builtin_nontemporal_store(T(0), pa + i0 + off);
+                    __builtin_nontemporal_store(T(0), pb + i0 + off);
+                }
+            }
+        }
+        return;
+    }
+    const unsigned used = (unsigned)(*g.cursor >> 32);
+    u64 who = ((u64)blockIdx.x * THREADS + threadIdx.x) >> lg;
+    if (WAVE) who = __builtin_amdgcn_readfirstlane((unsigned)who);   // below 2^32: MAX_BLOCKS blocks of 4 waves
+    for (; who < (u64)used * pieces; who += (u64)item_blocks * THREADS >> lg) {
+        const u64 index = who / pieces;
+        const unsigned c0 = (unsigned)(who - index * pieces) * ((unsigned)U << lg) + (threadIdx.x & ((1 << lg) - 1));
+        u64 c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            c[u] = c0 + ((u64)u << lg);
+            if (c[u] >= units) c[u] = units - 1;
+        }
+        const Item it = g.items[index];
+        RowSum<W> sum;
+        sum.template gather<WAVE>(ga, gb, g.list + it.first, it.count, D, c);
+        T *pa = reinterpret_cast<T*>(da + it.row * D), *pb = reinterpret_cast<T*>(db + it.row * D);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c0 + ((u64)u << lg) >= units) continue;
+            const T x = sum.a[u] * alpha, y = sum.b[u] * alpha;
+            if (!it.whole) { add_atomically(pa + c[u], x); add_atomically(pb + c[u], y); }
+            else if (accumulate) { pa[c[u]] += x; pb[c[u]] += y; }
+            else { __builtin_nontemporal_store(x, pa + c[u]); __builtin_nontemporal_store(y, pb + c[u]); }
+        }
+    }
+}
+
 const u64 MAX_COUNT = 0x7FFFFFFF;
+const u64 MAX_ROW = 1 << 22;          // words of a row: its accesses are counted in 32 bits, its pieces by the lookup's grid
+const u64 MAX_BLOCKS = 1 << 22;       // a grid has less than 2^32 threads; further rows are a block's next ones
 
 cg_status check_sizes(const void* ids, int id_bytes, size_t n, size_t V, size_t D) {
     if (V < 1 || D < 1 || (id_bytes != 4 && id_bytes != 8)) return CG_ERR_SHAPE;
     u64 words;
     if (__builtin_mul_overflow((u64)n, (u64)D, &words) || words > (SIZE_MAX >> 4)) return CG_ERR_SHAPE;
     if (__builtin_mul_overflow((u64)V, (u64)D, &words) || words > (SIZE_MAX >> 4)) return CG_ERR_SHAPE;
-    if (n > MAX_COUNT || V > MAX_COUNT || D > MAX_COUNT) return CG_ERR_UNSUPPORTED;
+    if (n > MAX_COUNT || V > MAX_COUNT || D > MAX_ROW) return CG_ERR_UNSUPPORTED;
     if (n > 0 && !ids) return CG_ERR_NULL;
     if (n > 0 && !aligned(ids, (size_t)id_bytes)) return CG_ERR_ALIGN;
     return CG_OK;
@@ -112,8 +432,62 @@ void launch_embed(const u64* ta, const u64* tb, const void* ids, u64 alpha, u64*
     const u64 units = D / W;
     const int lg = row_lanes_log2(units);
     const u64 rows = THREADS >> lg, piece = (u64)UNROLL << lg;
-    hipLaunchKernelGGL((embed_kernel<Id, W>), dim3((unsigned)((n + rows - 1) / rows), (unsigned)((units + piece - 1) / piece)),
+    const u64 blocks = (n + rows - 1) / rows;
+    hipLaunchKernelGGL((embed_kernel<Id, W>), dim3((unsigned)(blocks < MAX_BLOCKS ? blocks : MAX_BLOCKS), (unsigned)((units + piece - 1) / piece)),
                        dim3(THREADS), 0, s, ta, tb, static_cast<const Id*>(ids), alpha, za, zb, n, V, D, lg);
+}
+
+struct GradCall {
+    const u64 *ga, *gb;
+    const void* ids;
+    u64 alpha;
+    u64 *da, *db;
+    u64 n, V, D;
+    int accumulate;
+};
+
+unsigned blocks_of(u64 threads) { return (unsigned)((threads + THREADS - 1) / THREADS); }
+
+template <int W>
+void launch_sum(const GradCall& c, const Grouped& g, hipStream_t s) {
+    const int U = RowSum<W>::U;
+    const u64 units = c.D / W;
+    const int lg = row_lanes_log2((units + U - 1) / U);
+    const u64 piece = (u64)U << lg, pieces = (units + piece - 1) / piece, per_fill = (u64)FILL_ACCESSES * THREADS;
+    u64 items = ((g.items_max * pieces << lg) + THREADS - 1) / THREADS, fills = c.accumulate || g.one_block ? 0 : (c.V * units + per_fill - 1) / per_fill;
+    if (items > MAX_BLOCKS) items = MAX_BLOCKS;
+    if (fills > MAX_BLOCKS) fills = MAX_BLOCKS;
+    const dim3 grid((unsigned)(items + fills));
+    if (lg == 6)
+        hipLaunchKernelGGL((group_sum_kernel<W, true>), grid, dim3(THREADS), 0, s, c.ga, c.gb, c.alpha, c.da, c.db, c.V, c.D, c.accumulate, lg,
+                           (unsigned)pieces, (unsigned)items, g);
+    else
+        hipLaunchKernelGGL((group_sum_kernel<W, false>), grid, dim3(THREADS), 0, s, c.ga, c.gb, c.alpha, c.da, c.db, c.V, c.D, c.accumulate, lg,
+                           (unsigned)pieces, (unsigned)items, g);
+}
+
+template <class Id>
+void launch_grouped(const GradCall& c, bool vec, char* workspace, hipStream_t s) {
+    const Grouped g = grouped_layout(workspace, c.n, c.V);
+    const Id* ids = static_cast<const Id*>(c.ids);
+    const u64 words = c.V * c.D;
+    if (g.one_block) {
+        u64 blocks = c.accumulate ? 0 : (words + 8 * GROUP_THREADS - 1) / (8 * GROUP_THREADS);
+        if (blocks > 2048) blocks = 2048;
+        const bool pairs = aligned(c.da, 16) && aligned(c.db, 16) && words % 2 == 0;
+        hipLaunchKernelGGL(group_few_kernel<Id>, dim3(1 + (unsigned)blocks), dim3(GROUP_THREADS), 0, s, ids, c.n, c.V, g, c.da, c.db, words, pairs);
+        if (vec) launch_sum<2>(c, g, s);
+        else launch_sum<1>(c, g, s);
+        return;
+    }
+    const unsigned tokens = blocks_of(c.n), clears = blocks_of(c.V + 2);
+    const unsigned per_block = GROUP_THREADS * GROUP_TOKENS;
+    hipLaunchKernelGGL(group_clear_kernel, dim3(clears < 1024 ? clears : 1024), dim3(THREADS), 0, s, reinterpret_cast<unsigned*>(g.cursor), c.V + 2);
+    hipLaunchKernelGGL(group_count_kernel<Id>, dim3((unsigned)((c.n + per_block - 1) / per_block)), dim3(GROUP_THREADS), 0, s, ids, c.n, c.V, g);
+    hipLaunchKernelGGL(group_offset_kernel, dim3((unsigned)((c.V + GROUP_THREADS - 1) / GROUP_THREADS)), dim3(GROUP_THREADS), 0, s, c.V, g);
+    hipLaunchKernelGGL(group_list_kernel<Id>, dim3(tokens + (c.accumulate ? 0 : 512)), dim3(THREADS), 0, s, ids, c.n, c.V, c.D, g, tokens, c.da, c.db);
+    if (vec) launch_sum<2>(c, g, s);
+    else launch_sum<1>(c, g, s);
 }
 
 }  // namespace
@@ -132,7 +506,6 @@ cg_status cg_share_embedding(const uint64_t* ta, const uint64_t* tb, const void*
             return CG_ERR_ALIAS;
     if (overlap(za, zbytes, zb, zbytes)) return CG_ERR_ALIAS;
     const bool vec = D % 2 == 0 && all_aligned16(ptrs, 4);
-    if ((D / (vec ? 2 : 1) + 64 * UNROLL - 1) / (64 * UNROLL) > 65535) return CG_ERR_UNSUPPORTED;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (id_bytes == 8) {
         if (vec) launch_embed<long long, 2>(ta, tb, ids, alpha, za, zb, n, V, D, s);
@@ -144,23 +517,45 @@ cg_status cg_share_embedding(const uint64_t* ta, const uint64_t* tb, const void*
     return launched();
 }
 
+size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D) {
+    int id = 0;
+    if (n == 0 || check_sizes(&id, 4, n, V, D)) return 0;
+    return (size_t)grouped_layout(reinterpret_cast<char*>(256), n, V).bytes;
+}
+
 cg_status cg_share_embedding_grad(const uint64_t* ga, const uint64_t* gb, const void* ids, int id_bytes, uint64_t alpha,
                                   uint64_t* da, uint64_t* db, size_t n, size_t V, size_t D, int accumulate,
-                                  void* stream) {
+                                  void* workspace, size_t workspace_bytes, void* stream) {
     if (cg_status st = check_sizes(ids, id_bytes, n, V, D)) return st;
     if (accumulate != 0 && accumulate != 1) return CG_ERR_SHAPE;
     const void* out[2] = {da, db};
     if (cg_status st = check_ptrs(out, 2)) return st;
     const u64 dbytes = (u64)V * D * 8, gbytes = (u64)n * D * 8, ibytes = (u64)n * id_bytes;
     if (overlap(da, dbytes, db, dbytes)) return CG_ERR_ALIAS;
+    bool vec = D % 2 == 0 && all_aligned16(out, 2);
     if (n > 0) {
         const void* in[2] = {ga, gb};
         if (cg_status st = check_ptrs(in, 2)) return st;
         for (int o = 0; o < 2; ++o)
             if (overlap(out[o], dbytes, ga, gbytes) || overlap(out[o], dbytes, gb, gbytes) || overlap(out[o], dbytes, ids, ibytes))
                 return CG_ERR_ALIAS;
+        vec = vec && all_aligned16(in, 2);
+    }
+    const u64 need = cg_share_embedding_grad_workspace_bytes(n, V, D);
+    const bool scratch = need > 0 && workspace && workspace_bytes >= need && aligned(workspace, 16);
+    if (scratch) {
+        const void* operands[5] = {ga, gb, ids, da, db};
+        const u64 bytes[5] = {gbytes, gbytes, ibytes, dbytes, dbytes};
+        for (int k = 0; k < 5; ++k)
+            if (overlap(workspace, need, operands[k], bytes[k])) return CG_ERR_ALIAS;
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (scratch) {
+        const GradCall c = {ga, gb, ids, alpha, da, db, n, V, D, accumulate};
+        if (id_bytes == 8) launch_grouped<long long>(c, vec, static_cast<char*>(workspace), s);
+        else launch_grouped<int>(c, vec, static_cast<char*>(workspace), s);
+        return launched();
+    }
     if (!accumulate) hipLaunchKernelGGL(clear_kernel, dim3(2048), dim3(THREADS), 0, s, da, db, (u64)V * D);
     if (n > 0) {
         if (id_bytes == 8)

@@ -124,20 +124,25 @@ GRADS = [(1, 1, 1), (1, 700, 512), (2, 5, 3), (63, 7, 16), (64, 64, 64), (65, 10
 
 @pytest.mark.parametrize("n,V,D", GRADS)
 @pytest.mark.parametrize("kind", ["rank", "mixed", "one", "position"])
-def test_gradient(cg, ro, wl, n, V, D, kind):
-    say(f"gradient n={n} V={V} D={D} {kind}")
+@pytest.mark.parametrize("scratch", [True, False])
+def test_gradient(cg, ro, wl, n, V, D, kind, scratch):
+    say(f"gradient n={n} V={V} D={D} {kind}, scratch memory {scratch}")
     ids, alpha, words = draw_ids(kind, n, V, n + D), 0xFEDCBA9876543210 + n, int(kind == "mixed")
     G = [wl.draw_ring((n, D), 120 + k) for k in range(2)]
     dev = torch.from_numpy(ids).to("cuda").to(torch.int32 if kind == "rank" else torch.int64)
     g = [place(cg, t, words) for t in G]
     d = [Guarded((V, D), words) for _ in range(2)]
-    cg.cg_share_embedding_grad(*g, dev, V, alpha, da=d[0].t, db=d[1].t)
+    need = cg.cg_share_embedding_grad_workspace_bytes(n, V, D) if scratch else 0
+    memory = torch.full((need + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+    ws = memory[256:256 + need]                              # without: none of it is used
+    cg.cg_share_embedding_grad(*g, dev, V, alpha, da=d[0].t, db=d[1].t, workspace=ws)
     want = [ro.embedding_grad(t, ids, V, alpha) for t in G]
     for w, out in zip(want, d):
         assert np.array_equal(out.host(), w), first_mismatch(out.host(), w)
-    cg.cg_share_embedding_grad(*g, dev, V, alpha, da=d[0].t, db=d[1].t, accumulate=True)     # and once more on top
+    cg.cg_share_embedding_grad(*g, dev, V, alpha, da=d[0].t, db=d[1].t, accumulate=True, workspace=ws)     # and once more on top
     for w, out in zip(want, d):
         assert np.array_equal(out.host(), w + w), first_mismatch(out.host(), w + w)
+    assert bool((memory[:256] == 0x5A).all()) and bool((memory[256 + need:] == 0x5A).all())
 
 
 @pytest.mark.parametrize("n", [0, 40, 5000, 20000])
@@ -187,19 +192,21 @@ def test_gradient_in_two_graphs(cg, ro, wl, n):
     state, graphs = [], []
     for k in range(2):
         ids = torch.from_numpy(draw_ids("rank", n, V, k)).cuda()
+        # the second graph has scratch memory of its own, the first none
+        ws = torch.empty(cg.cg_share_embedding_grad_workspace_bytes(n, V, D) if k else 0, dtype=torch.uint8, device="cuda")
         g = [cg.to_device(wl.draw_ring((n, D), 160 + c)) for c in range(2)]
         d = [torch.zeros((V, D), dtype=torch.int64, device="cuda") for _ in range(2)]
-        cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1])
+        cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1], workspace=ws)
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
-            cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1])
-            cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1], accumulate=True)
-        state.append((ids, g, d))
+            cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1], workspace=ws)
+            cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1], accumulate=True, workspace=ws)
+        state.append((ids, g, d, ws))
         graphs.append(graph)
     for turn in range(4):
         for k in range(2):
-            ids, g, d = state[k]
+            ids, g, d, _ = state[k]
             host = draw_ids(["rank", "one", "mixed", "uniform"][turn], n, V, 10 * turn + k)
             G = [wl.draw_ring((n, D), 170 + 10 * turn + 2 * k + c) for c in range(2)]
             ids.copy_(torch.from_numpy(host))

@@ -34,6 +34,7 @@ def test_embedding_validation(b):
         assert call(**bad) == b.CG_ERR_SHAPE
     assert call(n=1 << 31, D=1) == b.CG_ERR_UNSUPPORTED
     assert call(V=1 << 31, D=1) == b.CG_ERR_UNSUPPORTED
+    assert call(D=(1 << 22) + 1) == b.CG_ERR_UNSUPPORTED
     for bad in (dict(za=P + 8), dict(zb=2 * P + 10 * 6 * 8 - 8), dict(za=5 * P), dict(za=5 * P + 4 * 6 * 8 - 8), dict(zb=3 * P + 24)):
         assert call(**bad) == b.CG_ERR_ALIAS
     assert call(n=0, ids=0, za=0, zb=0, ta=0, tb=0) == b.CG_OK
@@ -42,7 +43,7 @@ def test_embedding_validation(b):
 
 def test_embedding_gradient_validation(b):
     f = b.lib().cg_share_embedding_grad
-    ok = dict(ga=P, gb=2 * P, ids=3 * P, w=4, alpha=1, da=4 * P, db=5 * P, n=4, V=10, D=6, acc=0)
+    ok = dict(ga=P, gb=2 * P, ids=3 * P, w=4, alpha=1, da=4 * P, db=5 * P, n=4, V=10, D=6, acc=0, ws=0, bytes=0)
 
     def call(**kw):
         return f(*{**ok, **kw}.values(), None)
@@ -55,6 +56,13 @@ def test_embedding_gradient_validation(b):
     for bad in (dict(da=P), dict(db=2 * P + 4 * 6 * 8 - 8), dict(da=5 * P + 8), dict(da=3 * P + 8)):
         assert call(**bad) == b.CG_ERR_ALIAS
     assert call(n=0, acc=1, da=0) == b.CG_ERR_NULL
+    # scratch memory that would be used and lies in an operand
+    need = b.cg_share_embedding_grad_workspace_bytes
+    n, V, D = 20000, 500, 6
+    assert need(n, V, D) > 8 * n
+    for where in (P, 2 * P + n * D * 8 - 16, 3 * P + 16, 4 * P, 5 * P - need(n, V, D) + 16):
+        assert call(n=n, V=V, D=D, ws=where, bytes=need(n, V, D)) == b.CG_ERR_ALIAS
+    assert need(0, 5, 5) == need(5, 0, 5) == need(5, 5, 0) == need(1 << 31, 5, 5) == need(5, 5, (1 << 22) + 1) == 0
 
 
 def desc(b, **kw):
@@ -173,3 +181,17 @@ def test_binding_refuses_what_the_library_cannot_see(b, monkeypatch):
         b.ShareList([t], [t[:2]])
     with pytest.raises(ValueError):
         b.cg_clip_factor(t[0, :1], t[0, :1], t[0, :2], 1, 16)
+
+
+def test_small_scratch_is_taken_without_asking_how_much_is_free(b, monkeypatch):
+    asked, real_empty = [], torch.empty
+    monkeypatch.setattr(b, "_scratch_fits", lambda nbytes, device: asked.append(nbytes) or True)
+    monkeypatch.setattr(b, "_exchange_capture_mode", lambda mode: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch, "empty", lambda n, dtype=None, device=None: real_empty(n, dtype=dtype))
+    device = torch.device("cuda", 0)
+    assert b._scratch(b.SCRATCH_SMALL, device, None).numel() == b.SCRATCH_SMALL and asked == []
+    assert b._scratch(b.SCRATCH_SMALL + 1, device, None) is not None and asked == [b.SCRATCH_SMALL + 1]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    assert b._scratch(b.SCRATCH_SMALL, device, None) is None
