@@ -29,6 +29,7 @@ struct NormArgs {
     const u64 *a[NORM_MAX], *b[NORM_MAX];
     u64 n[NORM_MAX];
     unsigned first[NORM_MAX];   // block with the tensor's first chunk
+    unsigned keep_from;         // first block whose loads may stay in the caches
     int count;
 };
 
@@ -53,30 +54,73 @@ __device__ __forceinline__ int tensor_of(const Args& t, unsigned block) {
 
 __global__ void set_word_kernel(u64* z, u64 v) { *z = v; }
 
+const int NORM_UNROLL = 8;   // loads of each component under way per lane
+
+// Clipping reads what the norm has read, as soon as the factor is there.  The norm's last KEEP_WORDS elements (both
+// components, 192 MB of the 256 MB that the memory-side cache holds) are therefore read as what is wanted again, and
+// clipping begins at the end; what lies before them streams past the caches.  19.3 million elements: norm + clipping
+// 89 + 102 us with plain accesses from the beginning, 55 + 117 us with all of the norm streaming, 55 + 95 us this way.
+const u64 KEEP_WORDS = (u64)12 << 20;
+
+template <bool KEEP>
+__device__ __forceinline__ u64 load(const u64* p) {
+    return KEEP ? *p : __builtin_nontemporal_load(p);
+}
+
+template <bool KEEP>
+__device__ __forceinline__ u64 sum_of_squares(const u64* __restrict__ a, const u64* __restrict__ b, u64 i, u64 end) {
+    u64 sum = 0;
+    for (; i + (NORM_UNROLL - 1) * THREADS < end; i += NORM_UNROLL * THREADS) {
+        u64 x[NORM_UNROLL], y[NORM_UNROLL];
+#pragma unroll
+        for (int u = 0; u < NORM_UNROLL; ++u) { x[u] = load<KEEP>(a + i + u * THREADS); y[u] = load<KEEP>(b + i + u * THREADS); }
+#pragma unroll
+        for (int u = 0; u < NORM_UNROLL; ++u) sum += x[u] * (x[u] + 2 * y[u]);
+    }
+    for (; i < end; i += THREADS) sum += a[i] * (a[i] + 2 * b[i]);
+    return sum;
+}
+
 __global__ __launch_bounds__(THREADS) void sq_norm_kernel(NormArgs t, u64 chunk, u64* z) {
     const int k = tensor_of(t, blockIdx.x);
     const u64 begin = (u64)(blockIdx.x - t.first[k]) * chunk, end = begin + chunk < t.n[k] ? begin + chunk : t.n[k];
-    const u64 *a = t.a[k], *b = t.b[k];
-    u64 sum = 0;
-    for (u64 i = begin + threadIdx.x; i < end; i += THREADS) sum += a[i] * (a[i] + 2 * b[i]);
-    __shared__ u64 part[THREADS];
-    part[threadIdx.x] = sum;
+    u64 sum = blockIdx.x >= t.keep_from ? sum_of_squares<true>(t.a[k], t.b[k], begin + threadIdx.x, end)
+                                        : sum_of_squares<false>(t.a[k], t.b[k], begin + threadIdx.x, end);
+    for (int h = 32; h > 0; h >>= 1) sum += __shfl_xor((unsigned long long)sum, h);
+    __shared__ u64 part[THREADS / 64];
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
-    for (int h = THREADS / 2; h > 0; h >>= 1) {
-        if ((int)threadIdx.x < h) part[threadIdx.x] += part[threadIdx.x + h];
-        __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < THREADS / 64; ++w) sum += part[w];
+        atomicAdd(reinterpret_cast<unsigned long long*>(z), (unsigned long long)sum);
     }
-    if (threadIdx.x == 0) atomicAdd(reinterpret_cast<unsigned long long*>(z), (unsigned long long)part[0]);
 }
 
+const int CLIP_UNROLL = 4;
+
+// The list and every tensor's chunks from the end to the beginning (see KEEP_WORDS).
 __global__ __launch_bounds__(THREADS) void clip_kernel(ClipArgs t, u64 chunk, const u64* __restrict__ factor) {
     const int k = tensor_of(t, blockIdx.x);
-    const u64 begin = (u64)(blockIdx.x - t.first[k]) * chunk, end = begin + chunk < t.n[k] ? begin + chunk : t.n[k];
+    const u64 n = t.n[k], last = (n - 1) / chunk;
+    const u64 begin = (last - (blockIdx.x - t.first[k])) * chunk, end = begin + chunk < n ? begin + chunk : n;
     const u64 c = *factor;
-    for (u64 i = begin + threadIdx.x; i < end; i += THREADS) {
-        const u64 a = t.a[k][i], b = t.b[k][i];
-        t.za[k][i] = a * c;
-        t.zb[k][i] = b * c;
+    const u64 *a = t.a[k], *b = t.b[k];
+    u64 *za = t.za[k], *zb = t.zb[k];
+    u64 i = begin + threadIdx.x;
+    for (; i + (CLIP_UNROLL - 1) * THREADS < end; i += CLIP_UNROLL * THREADS) {
+        u64 x[CLIP_UNROLL], y[CLIP_UNROLL];
+#pragma unroll
+        for (int u = 0; u < CLIP_UNROLL; ++u) { x[u] = a[i + u * THREADS]; y[u] = b[i + u * THREADS]; }
+#pragma unroll
+        for (int u = 0; u < CLIP_UNROLL; ++u) {
+            __builtin_nontemporal_store(x[u] * c, za + i + u * THREADS);
+            __builtin_nontemporal_store(y[u] * c, zb + i + u * THREADS);
+        }
+    }
+    for (; i < end; i += THREADS) {
+        const u64 x = a[i], y = b[i];
+        za[i] = x * c;
+        zb[i] = y * c;
     }
 }
 
@@ -150,8 +194,8 @@ cg_status check_list(const u64* const* const* lists, int parts, const size_t* n,
 }
 
 // Words of a block's chunk: about `blocks` blocks together, and no less than what keeps one busy.
-u64 chunk_words(u64 total, u64 blocks) {
-    const u64 least = 4096, c = (total / blocks + 1023) / 1024 * 1024;
+u64 chunk_words(u64 total, u64 blocks, u64 least) {
+    const u64 c = (total / blocks + 1023) / 1024 * 1024;
     return c < least ? least : c;
 }
 
@@ -170,10 +214,12 @@ cg_status cg_share_sq_norm(const uint64_t* const* x_i, const uint64_t* const* x_
         if (n[k] > 0 && (cg::overlap(z_i, 8, x_i[k], n[k] * 8) || cg::overlap(z_i, 8, x_ip1[k], n[k] * 8))) return CG_ERR_ALIAS;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(set_word_kernel, dim3(1), dim3(1), 0, s, z_i, (u64)0);
-    const u64 chunk = chunk_words(total, 2048);
+    const u64 chunk = chunk_words(total, 2048, 1024);
+    u64 left = total;
     for (size_t k = 0; k < count;) {
         NormArgs t;
         t.count = 0;
+        t.keep_from = ~0u;
         u64 blocks = 0;
         for (; k < count && t.count < NORM_MAX; ++k) {
             if (n[k] == 0) continue;
@@ -181,7 +227,10 @@ cg_status cg_share_sq_norm(const uint64_t* const* x_i, const uint64_t* const* x_
             t.b[t.count] = x_ip1[k];
             t.n[t.count] = n[k];
             t.first[t.count++] = (unsigned)blocks;
+            if (t.keep_from == ~0u && left <= KEEP_WORDS + n[k])   // the tensor that holds the border, or the first one behind it
+                t.keep_from = (unsigned)(blocks + (left > KEEP_WORDS ? (left - KEEP_WORDS) / chunk : 0));
             blocks += (n[k] + chunk - 1) / chunk;
+            left -= n[k];
         }
         if (t.count > 0) hipLaunchKernelGGL(sq_norm_kernel, dim3((unsigned)blocks), dim3(THREADS), 0, s, t, chunk, z_i);
     }
@@ -210,12 +259,13 @@ cg_status cg_share_clip(const uint64_t* const* xa, const uint64_t* const* xb, co
     if (total == 0) return CG_OK;
     if (cg_status st = check_written(xa, xb, za, zb, n, count)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const u64 chunk = chunk_words(total, 16384);
-    for (size_t k = 0; k < count;) {
+    const u64 chunk = chunk_words(total, 16384, 1024);
+    for (size_t next = count; next > 0;) {
         ClipArgs t;
         t.count = 0;
         u64 blocks = 0;
-        for (; k < count && t.count < CLIP_MAX; ++k) {
+        for (; next > 0 && t.count < CLIP_MAX; --next) {
+            const size_t k = next - 1;
             if (n[k] == 0) continue;
             t.a[t.count] = xa[k];
             t.b[t.count] = xb[k];
