@@ -25,11 +25,6 @@ typedef uint64_t u64;
 
 const int THREADS = 256;
 
-__device__ __forceinline__ u64 wave_sum(u64 v) {
-    for (int h = 32; h > 0; h >>= 1) v += __shfl_xor((unsigned long long)v, h);
-    return v;
-}
-
 struct HeadParams {
     const u64 *ga, *gb, *xa, *xb, *ra, *rb, *cos, *sin;
     const void* pos;
@@ -38,62 +33,145 @@ struct HeadParams {
     int heads, dim, rot, frac, interleaved, pos64;
 };
 
-// One wave per head of a row, one pair of elements per lane and step.
-__global__ __launch_bounds__(THREADS) void sq_sum_kernel(HeadParams p) {
-    const u64 w = ((u64)blockIdx.x * THREADS + threadIdx.x) >> 6, lane = threadIdx.x & 63;
-    const u64 t = w / p.heads, h = w - t * p.heads;
-    if (t >= p.rows) return;
-    const u64 *a = p.xa + t * p.ld_x + h * p.dim, *b = p.xb + t * p.ld_x + h * p.dim;
-    u64 sum = 0;
-    for (u64 d = lane; d < (u64)p.dim; d += 64) sum += a[d] * (a[d] + 2 * b[d]);
-    sum = wave_sum(sum);
-    if (lane == 0) p.out[w] = sum;
+typedef unsigned long long ull2 __attribute__((ext_vector_type(2)));
+template <int W>
+struct Words { typedef ull2 type; };
+template <>
+struct Words<1> { typedef u64 type; };
+__device__ __forceinline__ u64 sum_of(u64 v) { return v; }
+__device__ __forceinline__ u64 sum_of(ull2 v) { return v.x + v.y; }
+
+// A group of 2^lg lanes per head, SQ_UNROLL accesses of W words per lane and component under way: 16 lanes for 128 elements,
+// so that a wave has four heads to load before the first sum.
+const int SQ_UNROLL = 4;
+
+template <int W>
+__global__ __launch_bounds__(THREADS) void sq_sum_kernel(HeadParams p, int lg) {
+    typedef typename Words<W>::type T;
+    const unsigned lane = threadIdx.x & ((1 << lg) - 1), units = (unsigned)p.dim / W;
+    for (u64 w = ((u64)blockIdx.x * THREADS + threadIdx.x) >> lg; w < p.rows * p.heads; w += (u64)gridDim.x * THREADS >> lg) {
+        const unsigned t = (unsigned)w / (unsigned)p.heads, h = (unsigned)w - t * (unsigned)p.heads;
+        const T *a = reinterpret_cast<const T*>(p.xa + t * p.ld_x + (u64)h * p.dim), *b = reinterpret_cast<const T*>(p.xb + t * p.ld_x + (u64)h * p.dim);
+        T sum = T(0);
+        for (unsigned i = lane; i < units; i += SQ_UNROLL << lg) {
+            T x[SQ_UNROLL], y[SQ_UNROLL];
+#pragma unroll
+            for (int u = 0; u < SQ_UNROLL; ++u) {
+                const unsigned c = i + (u << lg);
+                x[u] = y[u] = T(0);
+                if (c < units) { x[u] = __builtin_nontemporal_load(a + c); y[u] = __builtin_nontemporal_load(b + c); }
+            }
+#pragma unroll
+            for (int u = 0; u < SQ_UNROLL; ++u) sum += x[u] * (x[u] + 2 * y[u]);
+        }
+        u64 all = sum_of(sum);
+        for (int h2 = 1 << lg >> 1; h2 > 0; h2 >>= 1) all += __shfl_xor((unsigned long long)all, h2);
+        if (lane == 0) p.out[w] = all;
+    }
 }
 
-template <bool GRAD>
-__global__ __launch_bounds__(THREADS) void rotate_kernel(HeadParams p) {
-    const u64 w = ((u64)blockIdx.x * THREADS + threadIdx.x) >> 6, lane = threadIdx.x & 63;
-    const u64 t = w / p.heads, h = w - t * p.heads;
-    if (t >= p.rows) return;
-    const int half = p.rot / 2;
-    const u64 at = p.rot == 0 ? 0 : p.pos64 ? (u64) static_cast<const long long*>(p.pos)[t]
-                                            : (u64)(long long) static_cast<const int*>(p.pos)[t];
-    const bool there = p.rot == 0 || at < p.positions;
-    const u64 *xa = p.xa + t * p.ld_x + h * p.dim, *xb = p.xb + t * p.ld_x + h * p.dim;
-    const u64 *ga = GRAD ? p.ga + t * p.ld_g + h * p.dim : nullptr, *gb = GRAD ? p.gb + t * p.ld_g + h * p.dim : nullptr;
-    u64* out = p.out + t * p.ld_out + h * p.dim;
-    const u64 ra = p.ra[w], r2 = ra + p.rb[w], one = (u64)1 << p.frac;
-    u64 dr = 0;
-    const int items = half + (p.dim - p.rot);   // pairs to turn, then single elements
-    for (int i = (int)lane; i < items; i += 64) {
-        const bool pair = i < half;
-        const int d1 = !pair ? p.rot + (i - half) : p.interleaved ? 2 * i : i;
-        const int d2 = !pair ? d1 : p.interleaved ? 2 * i + 1 : i + half;
-        if (!there) {
-            out[d1] = 0;
-            out[d2] = 0;
-            continue;
-        }
-        const u64 c = pair ? p.cos[at * half + i] : one, s = pair ? p.sin[at * half + i] : 0;
-        if (!GRAD) {
-            const u64 u1 = xa[d1] * r2 + xb[d1] * ra, u2 = xa[d2] * r2 + xb[d2] * ra;
-            out[d1] = u1 * c - u2 * s;
-            if (pair) out[d2] = u1 * s + u2 * c;
+// The pair of a turn that lies at unit i of a head: W words each (two neighbouring pairs at a time where they lie half a
+// turn apart), or both words of one pair in one access where they lie next to each other.
+template <int W, bool INTER>
+struct Pairs {
+    typedef typename Words<INTER ? 1 : W>::type T;
+    static __device__ __forceinline__ void load(const u64* __restrict__ p, unsigned i, unsigned half, T* first, T* second) {
+        if (INTER && W == 2) {
+            const ull2 v = reinterpret_cast<const ull2*>(p)[i];
+            *first = v.x;
+            *second = v.y;
+        } else if (INTER) {
+            *first = p[2 * i];
+            *second = p[2 * i + 1];
         } else {
-            const u64 a1 = ga[d1], a2 = ga[d2], b1 = gb[d1], b2 = gb[d2];
-            const u64 va1 = a1 * c + a2 * s, vb1 = b1 * c + b2 * s;
-            out[d1] = va1 * r2 + vb1 * ra;
-            dr += xa[d1] * (va1 + vb1) + xb[d1] * va1;
-            if (pair) {
-                const u64 va2 = a2 * c - a1 * s, vb2 = b2 * c - b1 * s;
-                out[d2] = va2 * r2 + vb2 * ra;
-                dr += xa[d2] * (va2 + vb2) + xb[d2] * va2;
-            }
+            *first = reinterpret_cast<const T*>(p)[i];
+            *second = reinterpret_cast<const T*>(p + half)[i];
         }
     }
-    if (GRAD) {
-        dr = wave_sum(dr);
-        if (lane == 0) p.dr[w] = dr;
+    static __device__ __forceinline__ void store(u64* p, unsigned i, unsigned half, T first, T second) {
+        if (INTER && W == 2) {
+            ull2 v = {(unsigned long long)sum_of(first), (unsigned long long)sum_of(second)};
+            __builtin_nontemporal_store(v, reinterpret_cast<ull2*>(p) + i);
+        } else if (INTER) {
+            p[2 * i] = sum_of(first);
+            p[2 * i + 1] = sum_of(second);
+        } else {
+            __builtin_nontemporal_store(first, reinterpret_cast<T*>(p) + i);
+            __builtin_nontemporal_store(second, reinterpret_cast<T*>(p + half) + i);
+        }
+    }
+};
+
+// A group of 2^lg lanes per head: first the pairs that are turned, UNROLL units per lane under way, then the elements that
+// are only scaled.  Lanes behind the end read the last unit again and write nothing.  A position outside the table has
+// zeros for its angles and for the scale.
+template <bool GRAD, int W, bool INTER>
+__global__ __launch_bounds__(THREADS) void rotate_kernel(HeadParams p, int lg) {
+    typedef Pairs<W, INTER> P;
+    typedef typename P::T T;
+    typedef typename Words<W>::type S;
+    const int UNROLL = GRAD ? 1 : 2;
+    const unsigned lane = threadIdx.x & ((1 << lg) - 1), half = (unsigned)p.rot / 2;
+    const unsigned pairs = INTER ? half : half / W, singles = (unsigned)(p.dim - p.rot) / W;
+    for (u64 w = ((u64)blockIdx.x * THREADS + threadIdx.x) >> lg; w < p.rows * p.heads; w += (u64)gridDim.x * THREADS >> lg) {
+        const unsigned t = (unsigned)w / (unsigned)p.heads, h = (unsigned)w - t * (unsigned)p.heads;
+        const u64 *xa = p.xa + t * p.ld_x + (u64)h * p.dim, *xb = p.xb + t * p.ld_x + (u64)h * p.dim;
+        const u64 *ga = GRAD ? p.ga + t * p.ld_g + (u64)h * p.dim : nullptr, *gb = GRAD ? p.gb + t * p.ld_g + (u64)h * p.dim : nullptr;
+        u64* out = p.out + t * p.ld_out + (u64)h * p.dim;
+        u64 at = 0;
+        bool there = true;
+        if (half) {
+            at = p.pos64 ? (u64) static_cast<const long long*>(p.pos)[t] : (u64)(long long) static_cast<const int*>(p.pos)[t];
+            there = at < p.positions;
+            if (!there) at = 0;
+        }
+        const T *cos = reinterpret_cast<const T*>(p.cos + at * half), *sin = reinterpret_cast<const T*>(p.sin + at * half);
+        const u64 ra = p.ra[w], r2 = ra + p.rb[w];
+        u64 dr = 0;
+        for (unsigned i0 = lane; i0 < pairs; i0 += UNROLL << lg) {
+            T a1[UNROLL], a2[UNROLL], b1[UNROLL], b2[UNROLL], c[UNROLL], s[UNROLL];
+            T xa1[UNROLL], xa2[UNROLL], xb1[UNROLL], xb2[UNROLL];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const unsigned i = i0 + (u << lg) < pairs ? i0 + (u << lg) : pairs - 1;
+                P::load(GRAD ? ga : xa, i, half, &a1[u], &a2[u]);
+                P::load(GRAD ? gb : xb, i, half, &b1[u], &b2[u]);
+                if (GRAD) {
+                    P::load(xa, i, half, &xa1[u], &xa2[u]);
+                    P::load(xb, i, half, &xb1[u], &xb2[u]);
+                }
+                c[u] = cos[i];
+                s[u] = sin[i];
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const unsigned i = i0 + (u << lg);
+                if (i >= pairs) continue;
+                if (!there) c[u] = s[u] = T(0);
+                if (!GRAD) {
+                    const T u1 = a1[u] * r2 + b1[u] * ra, u2 = a2[u] * r2 + b2[u] * ra;
+                    P::store(out, i, half, u1 * c[u] - u2 * s[u], u1 * s[u] + u2 * c[u]);
+                } else {
+                    const T va1 = a1[u] * c[u] + a2[u] * s[u], va2 = a2[u] * c[u] - a1[u] * s[u];
+                    const T vb1 = b1[u] * c[u] + b2[u] * s[u], vb2 = b2[u] * c[u] - b1[u] * s[u];
+                    P::store(out, i, half, va1 * r2 + vb1 * ra, va2 * r2 + vb2 * ra);
+                    dr += sum_of(xa1[u] * (va1 + vb1) + xb1[u] * va1 + xa2[u] * (va2 + vb2) + xb2[u] * va2);
+                }
+            }
+        }
+        for (unsigned i = lane; i < singles; i += 1 << lg) {
+            const S va = reinterpret_cast<const S*>((GRAD ? ga : xa) + p.rot)[i] * ((u64)there << p.frac);
+            const S vb = reinterpret_cast<const S*>((GRAD ? gb : xb) + p.rot)[i] * ((u64)there << p.frac);
+            __builtin_nontemporal_store(va * r2 + vb * ra, reinterpret_cast<S*>(out + p.rot) + i);
+            if (GRAD) {
+                const S x = reinterpret_cast<const S*>(xa + p.rot)[i], y = reinterpret_cast<const S*>(xb + p.rot)[i];
+                dr += sum_of(x * (va + vb) + y * va);
+            }
+        }
+        if (GRAD) {
+            for (int o = 1 << lg >> 1; o > 0; o >>= 1) dr += __shfl_xor((unsigned long long)dr, o);
+            if (lane == 0) p.dr[w] = dr;
+        }
     }
 }
 
@@ -156,7 +234,37 @@ bool meets_inputs(const void* out, u64 bytes, const void* const* in, const u64* 
     return false;
 }
 
-unsigned wave_blocks(u64 waves) { return (unsigned)((waves + THREADS / 64 - 1) / (THREADS / 64)); }
+// 2^lg lanes, up to a wave, for `units` accesses, `each` per lane
+int lanes_log2(int64_t units, int each) {
+    int lg = 0;
+    while (lg < 6 && ((int64_t)each << lg) < units) ++lg;
+    return lg;
+}
+
+// Blocks for `groups` groups of 2^lg lanes: a grid has less than 2^32 threads, further groups are a block's next ones.
+dim3 group_blocks(u64 groups, int lg) {
+    const u64 blocks = ((groups << lg) + THREADS - 1) / THREADS, most = 1 << 22;
+    return dim3((unsigned)(blocks < most ? blocks : most));
+}
+
+template <bool GRAD, int W>
+void launch_rotate(const HeadParams& p, hipStream_t s) {
+    const int64_t pairs = p.interleaved ? p.rot / 2 : p.rot / 2 / W, singles = (p.dim - p.rot) / W;
+    const int lg = pairs > singles ? lanes_log2(pairs, GRAD ? 1 : 2) : lanes_log2(singles, 1);
+    const dim3 grid = group_blocks(p.rows * p.heads, lg);
+    if (p.interleaved) hipLaunchKernelGGL((rotate_kernel<GRAD, W, true>), grid, dim3(THREADS), 0, s, p, lg);
+    else hipLaunchKernelGGL((rotate_kernel<GRAD, W, false>), grid, dim3(THREADS), 0, s, p, lg);
+}
+
+// 16-byte accesses where everything that is read or written that way begins and goes on in whole pairs of words.
+template <bool GRAD>
+void launch_rotate(const HeadParams& p, void* stream) {
+    const void* ptrs[7] = {p.xa, p.xb, p.out, p.ga, p.gb, p.cos, p.sin};
+    bool vec = (p.dim | p.rot | (int)((p.ld_x | p.ld_g | p.ld_out) & 1)) % 2 == 0 && (p.interleaved || p.rot % 4 == 0);
+    for (int i = 0; i < (p.rot > 0 && !p.interleaved ? 7 : 5); ++i) vec = vec && aligned(ptrs[i], 16);
+    if (vec) launch_rotate<GRAD, 2>(p, static_cast<hipStream_t>(stream));
+    else launch_rotate<GRAD, 1>(p, static_cast<hipStream_t>(stream));
+}
 
 cg_status launched() { return hipGetLastError() == hipSuccess ? CG_OK : CG_ERR_DEVICE; }
 
@@ -176,7 +284,11 @@ cg_status cg_share_head_sq_sum(const uint64_t* x_i, const uint64_t* x_ip1, uint6
     HeadParams p = {};
     p.xa = x_i; p.xb = x_ip1; p.out = z_i;
     p.rows = (u64)rows; p.ld_x = (u64)ld_x; p.heads = (int)heads; p.dim = (int)dim;
-    hipLaunchKernelGGL(sq_sum_kernel, dim3(wave_blocks(p.rows * p.heads)), dim3(THREADS), 0, static_cast<hipStream_t>(stream), p);
+    const bool vec = dim % 2 == 0 && ld_x % 2 == 0 && aligned(x_i, 16) && aligned(x_ip1, 16);
+    const int lg = lanes_log2(dim / (vec ? 2 : 1), SQ_UNROLL);
+    const dim3 grid = group_blocks(p.rows * p.heads, lg);
+    if (vec) hipLaunchKernelGGL(sq_sum_kernel<2>, grid, dim3(THREADS), 0, static_cast<hipStream_t>(stream), p, lg);
+    else hipLaunchKernelGGL(sq_sum_kernel<1>, grid, dim3(THREADS), 0, static_cast<hipStream_t>(stream), p, lg);
     return launched();
 }
 
@@ -195,7 +307,7 @@ cg_status cg_share_head_norm_rotate(const uint64_t* x_i, const uint64_t* x_ip1, 
                              d->rot ? (u64)d->rows * d->pos_bytes : 0};
     if (meets_inputs(z_i, zbytes, in, in_bytes, 7)) return CG_ERR_ALIAS;
     const HeadParams p = head_params(x_i, x_ip1, r_i, r_ip1, cos, sin, pos, z_i, d);
-    hipLaunchKernelGGL(rotate_kernel<false>, dim3(wave_blocks(p.rows * p.heads)), dim3(THREADS), 0, static_cast<hipStream_t>(stream), p);
+    launch_rotate<false>(p, stream);
     return launched();
 }
 
@@ -219,7 +331,7 @@ cg_status cg_share_head_norm_rotate_grad(const uint64_t* g_i, const uint64_t* g_
         return CG_ERR_ALIAS;
     HeadParams p = head_params(x_i, x_ip1, r_i, r_ip1, cos, sin, pos, dx_i, d);
     p.ga = g_i; p.gb = g_ip1; p.dr = dr_i;
-    hipLaunchKernelGGL(rotate_kernel<true>, dim3(wave_blocks(p.rows * p.heads)), dim3(THREADS), 0, static_cast<hipStream_t>(stream), p);
+    launch_rotate<true>(p, stream);
     return launched();
 }
 
