@@ -176,6 +176,15 @@ def _current(*tensors) -> None:
             raise ValueError(f"tensors must live on the current GPU ({d}), got one on {t.device}")
 
 
+_INT64 = torch.int64
+
+
+def _ptrs(*tensors) -> list:
+    """Addresses of contiguous ring tensors on the current device."""
+    _current(*tensors)
+    return [t.data_ptr() if t.dtype is _INT64 and t.is_contiguous() else _ptr(t) for t in tensors]
+
+
 def _check(status: int, where: str) -> None:
     if status != CG_OK:
         raise CgError(status, where)
@@ -647,11 +656,13 @@ def cg_share_col_sum(xa, xb, za=None, zb=None, stream=None):
 
 def _index_ptr(t: torch.Tensor) -> Tuple[int, int]:
     """Address and bytes per entry of a tensor of ids or positions."""
-    if t.dtype not in (torch.int64, torch.int32):
+    width = {torch.int64: 8, torch.int32: 4}.get(t.dtype)
+    if width is None:
         raise TypeError(f"ids and positions are torch.int64 or torch.int32, got {t.dtype}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("ids and positions must be contiguous and live on the GPU")
-    return t.data_ptr(), 8 if t.dtype == torch.int64 else 4
+    _current(t)
+    if not t.is_contiguous():
+        raise ValueError("ids and positions must be contiguous")
+    return t.data_ptr(), width
 
 
 def cg_share_embedding(ta, tb, ids, alpha: int = 1, za=None, zb=None, stream=None):
@@ -663,12 +674,12 @@ def cg_share_embedding(ta, tb, ids, alpha: int = 1, za=None, zb=None, stream=Non
     shape = (*ids.shape, D)
     za = torch.empty(shape, dtype=torch.int64, device=ta.device) if za is None else za
     zb = torch.empty(shape, dtype=torch.int64, device=ta.device) if zb is None else zb
-    if tuple(za.shape) != shape or tuple(zb.shape) != shape:
+    if za.shape != shape or zb.shape != shape:
         raise ValueError("output shape does not match")
-    _current(ta, tb, ids, za, zb)
+    pta, ptb, pza, pzb = _ptrs(ta, tb, za, zb)
     ip, width = _index_ptr(ids)
-    _check(lib().cg_share_embedding(_ptr(ta), _ptr(tb), ip, width, int(alpha) % (1 << 64), _ptr(za), _ptr(zb), ids.numel(), V, D,
-                                    _stream(stream)), "cg_share_embedding")
+    _check(lib().cg_share_embedding(pta, ptb, ip, width, int(alpha) % (1 << 64), pza, pzb, ids.numel(), V, D, _stream(stream)),
+           "cg_share_embedding")
     return za, zb
 
 
@@ -684,15 +695,15 @@ def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=Non
         raise ValueError("accumulate needs the tensors to add to")
     da = torch.empty((V, D), dtype=torch.int64, device=ga.device) if da is None else da
     db = torch.empty((V, D), dtype=torch.int64, device=ga.device) if db is None else db
-    if tuple(da.shape) != (V, D) or tuple(db.shape) != (V, D):
+    if da.shape != (V, D) or db.shape != (V, D):
         raise ValueError("output shape does not match")
-    _current(ga, gb, ids, da, db)
+    pga, pgb, pda, pdb = _ptrs(ga, gb, da, db)
     ip, width = _index_ptr(ids)
     n = ids.numel()
     if workspace is None:
         workspace = _scratch(lib().cg_share_embedding_grad_workspace_bytes(n, V, D), ga.device, stream)
     wp, wb = _ws(workspace)
-    _check(lib().cg_share_embedding_grad(_ptr(ga), _ptr(gb), ip, width, int(alpha) % (1 << 64), _ptr(da), _ptr(db), n, V, D,
+    _check(lib().cg_share_embedding_grad(pga, pgb, ip, width, int(alpha) % (1 << 64), pda, pdb, n, V, D,
                                          int(bool(accumulate)), wp, wb, _stream(stream)), "cg_share_embedding_grad")
     return da, db
 
@@ -701,53 +712,51 @@ def cg_share_embedding_grad_workspace_bytes(n: int, V: int, D: int) -> int:
     return int(lib().cg_share_embedding_grad_workspace_bytes(n, V, D))
 
 
-def _head_rows(t: torch.Tensor, shape=None) -> Tuple[int, int]:
-    """Address and words from a row to the next of a [rows, heads, dim] tensor whose rows are whole but may lie apart."""
-    if t.dtype != torch.int64:
-        raise TypeError(f"ring tensors are torch.int64 (uint64 bit patterns), got {t.dtype}")
-    if t.dim() != 3 or (shape is not None and t.shape != shape):
+def _head_rows(a: torch.Tensor, *others) -> Tuple[int, list]:
+    """Words from a row to the next, and the addresses, of [rows, heads, dim] tensors whose rows are whole but may lie apart: the
+    components of a pair, alike."""
+    _current(a, *others)
+    shape, stride = a.shape, a.stride()
+    for t in (a, *others):
+        if t.dtype is not _INT64:
+            raise TypeError(f"ring tensors are torch.int64 (uint64 bit patterns), got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError("heads must be [rows, heads, dim] tensors of one shape")
+        if t.stride() != stride:
+            raise ValueError("both components must have their rows equally far apart")
+    if len(shape) != 3:
         raise ValueError("heads must be [rows, heads, dim] tensors of one shape")
-    rows, heads, dim = t.shape
-    step, head, one = t.stride()
-    if (dim > 1 and one != 1) or (heads > 1 and head != dim):
+    rows, heads, dim = shape
+    step, head, one = stride
+    if (one != 1 and dim > 1) or (head != dim and heads > 1):
         raise ValueError("the heads of a row must lie next to each other")
-    return t.data_ptr(), step if rows > 1 else heads * dim
-
-
-def _head_pair(a, b, shape=None) -> Tuple[int, int, int]:
-    (pa, ld), (pb, ld_b) = _head_rows(a, shape), _head_rows(b, a.shape)
-    if ld != ld_b:
-        raise ValueError("both components must have their rows equally far apart")
-    return pa, pb, ld
+    return step if rows > 1 else heads * dim, [t.data_ptr() for t in (a, *others)]
 
 
 def cg_share_head_sq_sum(x_i, x_ip1, z_i=None, stream=None) -> torch.Tensor:
     """z_i [rows, heads]: the party's additive share of each head's sum of squares; x [rows, heads, dim], a slice of wider rows
     (packed queries, keys and values) as it is."""
-    pa, pb, ld = _head_pair(x_i, x_ip1)
+    ld, px = _head_rows(x_i, x_ip1)
     rows, heads, dim = x_i.shape
     z_i = torch.empty((rows, heads), dtype=torch.int64, device=x_i.device) if z_i is None else z_i
-    if tuple(z_i.shape) != (rows, heads):
+    if z_i.shape != (rows, heads):
         raise ValueError("output shape does not match")
-    _current(x_i, x_ip1, z_i)
-    _check(lib().cg_share_head_sq_sum(pa, pb, _ptr(z_i), rows, heads, dim, ld, _stream(stream)), "cg_share_head_sq_sum")
+    _check(lib().cg_share_head_sq_sum(*px, *_ptrs(z_i), rows, heads, dim, ld, _stream(stream)), "cg_share_head_sq_sum")
     return z_i
 
 
 def _head_desc(x_i, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved):
     """The descriptor, and the addresses of the shared norms, of the angles and of the positions."""
     rows, heads, dim = x_i.shape
-    if tuple(r_i.shape) != (rows, heads) or r_ip1.shape != r_i.shape:
+    if r_i.shape != (rows, heads) or r_ip1.shape != (rows, heads):
         raise ValueError("the norms must be a pair of [rows, heads] tensors")
-    _current(x_i, r_i, r_ip1)
     if cos is None and sin is None and pos is None:
-        return HeadDesc(rows, heads, dim, 0, ld_x, ld_g, ld_out, 0, 8, frac_bits, int(bool(interleaved))), (_ptr(r_i), _ptr(r_ip1), 0, 0, 0)
-    if cos is None or sin is None or pos is None or cos.dim() != 2 or sin.shape != cos.shape or tuple(pos.shape) != (rows,):
+        return HeadDesc(rows, heads, dim, 0, ld_x, ld_g, ld_out, 0, 8, frac_bits, bool(interleaved)), (*_ptrs(r_i, r_ip1), 0, 0, 0)
+    if cos is None or sin is None or pos is None or cos.dim() != 2 or sin.shape != cos.shape or pos.shape != (rows,):
         raise ValueError("angles are a pair of [positions, rot / 2] tensors, with a position for each row")
-    _current(cos, sin, pos)
     pp, width = _index_ptr(pos)
-    d = HeadDesc(rows, heads, dim, 2 * cos.shape[1], ld_x, ld_g, ld_out, cos.shape[0], width, frac_bits, int(bool(interleaved)))
-    return d, (_ptr(r_i), _ptr(r_ip1), _ptr(cos), _ptr(sin), pp)
+    d = HeadDesc(rows, heads, dim, 2 * cos.shape[1], ld_x, ld_g, ld_out, cos.shape[0], width, frac_bits, bool(interleaved))
+    return d, (*_ptrs(r_i, r_ip1, cos, sin), pp)
 
 
 def cg_share_head_norm_rotate(x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=None, frac_bits: int = 0, interleaved: bool = False,
@@ -755,12 +764,13 @@ def cg_share_head_norm_rotate(x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=No
     """z_i [rows, heads, dim]: three-term product of each head with its shared inverse norm r [rows, heads], the first
     rot = 2 * cos.shape[1] elements turned by the public angles of the row's position, the others times 2^frac_bits.  Without
     angles the product alone, times 2^frac_bits."""
-    pa, pb, ld_x = _head_pair(x_i, x_ip1)
+    ld_x, px = _head_rows(x_i, x_ip1)
     z_i = torch.empty(x_i.shape, dtype=torch.int64, device=x_i.device) if z_i is None else z_i
-    pz, ld_out = _head_rows(z_i, x_i.shape)
-    _current(x_ip1, z_i)
+    ld_out, pz = _head_rows(z_i)
+    if z_i.shape != x_i.shape:
+        raise ValueError("output shape does not match")
     d, rest = _head_desc(x_i, ld_x, 0, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved)
-    _check(lib().cg_share_head_norm_rotate(pa, pb, *rest, pz, ctypes.byref(d), _stream(stream)), "cg_share_head_norm_rotate")
+    _check(lib().cg_share_head_norm_rotate(*px, *rest, *pz, ctypes.byref(d), _stream(stream)), "cg_share_head_norm_rotate")
     return z_i
 
 
@@ -768,17 +778,15 @@ def cg_share_head_norm_rotate_grad(g_i, g_ip1, x_i, x_ip1, r_i, r_ip1, cos=None,
                                    interleaved: bool = False, dx_i=None, dr_i=None, stream=None):
     """(dx_i [rows, heads, dim], dr_i [rows, heads]): the party's additive shares of the gradients with respect to the heads and
     to their inverse norms, from the gradient pair g of cg_share_head_norm_rotate's result."""
-    pa, pb, ld_x = _head_pair(x_i, x_ip1)
-    qa, qb, ld_g = _head_pair(g_i, g_ip1, x_i.shape)
-    rows, heads, _ = x_i.shape
+    ld_x, px = _head_rows(x_i, x_ip1)
+    ld_g, pg = _head_rows(g_i, g_ip1)
     dx_i = torch.empty(x_i.shape, dtype=torch.int64, device=x_i.device) if dx_i is None else dx_i
-    dr_i = torch.empty((rows, heads), dtype=torch.int64, device=x_i.device) if dr_i is None else dr_i
-    pd, ld_out = _head_rows(dx_i, x_i.shape)
-    if tuple(dr_i.shape) != (rows, heads):
-        raise ValueError("output shape does not match")
-    _current(x_ip1, g_i, g_ip1, dx_i, dr_i)
+    dr_i = torch.empty(x_i.shape[:2], dtype=torch.int64, device=x_i.device) if dr_i is None else dr_i
+    ld_out, pd = _head_rows(dx_i)
+    if not (g_i.shape == x_i.shape == dx_i.shape) or dr_i.shape != x_i.shape[:2]:
+        raise ValueError("operand shapes do not match")
     d, rest = _head_desc(x_i, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved)
-    _check(lib().cg_share_head_norm_rotate_grad(qa, qb, pa, pb, *rest, pd, _ptr(dr_i), ctypes.byref(d), _stream(stream)),
+    _check(lib().cg_share_head_norm_rotate_grad(*pg, *px, *rest, *pd, *_ptrs(dr_i), ctypes.byref(d), _stream(stream)),
            "cg_share_head_norm_rotate_grad")
     return dx_i, dr_i
 
@@ -806,8 +814,8 @@ def cg_share_sq_norm(x: ShareList, z_i=None, stream=None) -> torch.Tensor:
         z_i = torch.empty((1,), dtype=torch.int64, device=x.a[0].device if x.count else "cuda")
     elif z_i.numel() != 1:
         raise ValueError("output shape does not match")
-    _current(z_i, *x.a[:1])
-    _check(lib().cg_share_sq_norm(x.pa, x.pb, x.n, x.count, _ptr(z_i), _stream(stream)), "cg_share_sq_norm")
+    _current(*x.a[:1])
+    _check(lib().cg_share_sq_norm(x.pa, x.pb, x.n, x.count, *_ptrs(z_i), _stream(stream)), "cg_share_sq_norm")
     return z_i
 
 
@@ -819,8 +827,8 @@ def cg_clip_factor(s0, s1, s2, max_norm: int, frac_bits: int, factor=None, strea
         raise ValueError("the shares of the squared norm and the factor are one word each")
     if not 0 <= int(max_norm) < 1 << 64:
         raise ValueError("max_norm is a non-negative word")
-    _current(s0, s1, s2, factor)
-    _check(lib().cg_clip_factor(_ptr(s0), _ptr(s1), _ptr(s2), int(max_norm), frac_bits, _ptr(factor), _stream(stream)), "cg_clip_factor")
+    p0, p1, p2, pf = _ptrs(s0, s1, s2, factor)
+    _check(lib().cg_clip_factor(p0, p1, p2, int(max_norm), frac_bits, pf, _stream(stream)), "cg_clip_factor")
     return factor
 
 
@@ -829,8 +837,8 @@ def cg_share_clip(x: ShareList, factor, out: Optional[ShareList] = None, stream=
     out = x if out is None else out
     if out.shapes != x.shapes or factor.numel() != 1:
         raise ValueError("operand shapes do not match")
-    _current(factor, *x.a[:1], *out.a[:1])
-    _check(lib().cg_share_clip(x.pa, x.pb, _ptr(factor), out.pa, out.pb, x.n, x.count, _stream(stream)), "cg_share_clip")
+    _current(*x.a[:1], *out.a[:1])
+    _check(lib().cg_share_clip(x.pa, x.pb, *_ptrs(factor), out.pa, out.pb, x.n, x.count, _stream(stream)), "cg_share_clip")
     return out
 
 

@@ -305,6 +305,11 @@ struct RowSum {
     static const int R = W == 2 ? 4 : 2;
     T a[U], b[U];
 
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int u = 0; u < U; ++u) a[u] = b[u] = T(0);
+    }
+
     template <int N>
     __device__ __forceinline__ void add(const u64* __restrict__ ga, const u64* __restrict__ gb, const unsigned (&row)[N],
                                         u64 D, const u64 (&c)[U]) {
@@ -325,8 +330,7 @@ struct RowSum {
     template <bool WAVE>
     __device__ __forceinline__ void gather(const u64* __restrict__ ga, const u64* __restrict__ gb,
                                            const unsigned* __restrict__ list, unsigned count, u64 D, const u64 (&c)[U]) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) a[u] = b[u] = T(0);
+        clear();
         unsigned mine = 0;
         const int lane = threadIdx.x & 63;
         if (WAVE && lane < (int)count) mine = list[lane];
@@ -437,6 +441,73 @@ void launch_embed(const u64* ta, const u64* tb, const void* ids, u64 alpha, u64*
                        dim3(THREADS), 0, s, ta, tb, static_cast<const Id*>(ids), alpha, za, zb, n, V, D, lg);
 }
 
+// ---- gradient of a handful of tokens: one launch, no scratch memory ----
+// Every wave holds all ids, FEW / 64 per lane, and takes pieces of rows in turn: a ballot names the row's tokens.  Without
+// any the piece is a store of zeros.  Accumulating, the rows are those of the tokens instead, each by its first one.
+const u64 FEW = 128;
+
+template <class Id, int W>
+__global__ __launch_bounds__(THREADS) void few_sum_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
+                                                          const Id* __restrict__ ids, u64 alpha, u64* da, u64* db, u64 n, u64 V,
+                                                          u64 D, int accumulate, unsigned pieces) {
+    typedef typename Words<W>::type T;
+    const int U = RowSum<W>::U, lane = threadIdx.x & 63;
+    const unsigned units = (unsigned)(D / W);
+    u64 id[FEW / 64];
+#pragma unroll
+    for (int k = 0; k < (int)(FEW / 64); ++k) {
+        const u64 j = lane + 64 * k;
+        id[k] = j < n ? (u64)(long long)ids[j] : ~(u64)0;
+    }
+    const u64 all = (accumulate ? n : V) * pieces, step = (u64)gridDim.x * (THREADS / 64);
+    for (u64 q = (u64)blockIdx.x * (THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); q < all; q += step) {
+        u64 row = q / pieces;
+        const unsigned c0 = (unsigned)(q - row * pieces) * (U * 64) + lane, token = (unsigned)row;
+        if (accumulate) {
+            row = (u64)(long long)ids[token];
+            if (row >= V) continue;
+        }
+        u64 who[FEW / 64];
+        unsigned count = 0;
+#pragma unroll
+        for (int k = 0; k < (int)(FEW / 64); ++k) {
+            who[k] = __ballot(id[k] == row);
+            count += __popcll(who[k]);
+        }
+        if (accumulate && token != (who[0] ? (unsigned)__builtin_ctzll(who[0]) : 64 + (unsigned)__builtin_ctzll(who[1]))) continue;
+        u64 c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) c[u] = c0 + u * 64 < units ? c0 + u * 64 : units - 1;
+        RowSum<W> sum;
+        sum.clear();
+        const auto next = [&]() {
+            const int k = who[0] ? 0 : 1;
+            const unsigned j = 64 * k + (unsigned)__builtin_ctzll(who[k]);
+            who[k] &= who[k] - 1;
+            return j;
+        };
+        for (; count >= RowSum<W>::R; count -= RowSum<W>::R) {
+            unsigned j[RowSum<W>::R];
+#pragma unroll
+            for (int r = 0; r < RowSum<W>::R; ++r) j[r] = next();
+            sum.add(ga, gb, j, D, c);
+        }
+        for (; count > 0; --count) {
+            const unsigned j[1] = {next()};
+            sum.add(ga, gb, j, D, c);
+        }
+        T *pa = reinterpret_cast<T*>(da + row * D), *pb = reinterpret_cast<T*>(db + row * D);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c0 + u * 64 >= units) continue;
+            const T x = sum.a[u] * alpha, y = sum.b[u] * alpha;
+            if (accumulate) { pa[c[u]] += x; pb[c[u]] += y; }
+            else { __builtin_nontemporal_store(x, pa + c[u]); __builtin_nontemporal_store(y, pb + c[u]); }
+        }
+    }
+}
+static_assert(FEW == 128, "two ballots");
+
 struct GradCall {
     const u64 *ga, *gb;
     const void* ids;
@@ -464,6 +535,15 @@ void launch_sum(const GradCall& c, const Grouped& g, hipStream_t s) {
     else
         hipLaunchKernelGGL((group_sum_kernel<W, false>), grid, dim3(THREADS), 0, s, c.ga, c.gb, c.alpha, c.da, c.db, c.V, c.D, c.accumulate, lg,
                            (unsigned)pieces, (unsigned)items, g);
+}
+
+template <class Id, int W>
+void launch_few(const GradCall& c, hipStream_t s) {
+    const u64 piece = RowSum<W>::U * 64, pieces = (c.D / W + piece - 1) / piece;
+    const u64 waves = (c.accumulate ? c.n : c.V) * pieces;
+    const unsigned blocks = (unsigned)(waves < 4 * 2048 ? (waves + 3) / 4 : 2048);
+    hipLaunchKernelGGL((few_sum_kernel<Id, W>), dim3(blocks), dim3(THREADS), 0, s, c.ga, c.gb, static_cast<const Id*>(c.ids), c.alpha, c.da, c.db,
+                       c.n, c.V, c.D, c.accumulate, (unsigned)pieces);
 }
 
 template <class Id>
@@ -519,7 +599,7 @@ cg_status cg_share_embedding(const uint64_t* ta, const uint64_t* tb, const void*
 
 size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D) {
     int id = 0;
-    if (n == 0 || check_sizes(&id, 4, n, V, D)) return 0;
+    if (n <= FEW || check_sizes(&id, 4, n, V, D)) return 0;
     return (size_t)grouped_layout(reinterpret_cast<char*>(256), n, V).bytes;
 }
 
@@ -550,8 +630,18 @@ cg_status cg_share_embedding_grad(const uint64_t* ga, const uint64_t* gb, const 
             if (overlap(workspace, need, operands[k], bytes[k])) return CG_ERR_ALIAS;
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const GradCall c = {ga, gb, ids, alpha, da, db, n, V, D, accumulate};
+    if (n > 0 && n <= FEW) {
+        if (id_bytes == 8) {
+            if (vec) launch_few<long long, 2>(c, s);
+            else launch_few<long long, 1>(c, s);
+        } else {
+            if (vec) launch_few<int, 2>(c, s);
+            else launch_few<int, 1>(c, s);
+        }
+        return launched();
+    }
     if (scratch) {
-        const GradCall c = {ga, gb, ids, alpha, da, db, n, V, D, accumulate};
         if (id_bytes == 8) launch_grouped<long long>(c, vec, static_cast<char*>(workspace), s);
         else launch_grouped<int>(c, vec, static_cast<char*>(workspace), s);
         return launched();

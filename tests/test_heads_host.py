@@ -62,7 +62,8 @@ def test_embedding_gradient_validation(b):
     assert need(n, V, D) > 8 * n
     for where in (P, 2 * P + n * D * 8 - 16, 3 * P + 16, 4 * P, 5 * P - need(n, V, D) + 16):
         assert call(n=n, V=V, D=D, ws=where, bytes=need(n, V, D)) == b.CG_ERR_ALIAS
-    assert need(0, 5, 5) == need(5, 0, 5) == need(5, 5, 0) == need(1 << 31, 5, 5) == need(5, 5, (1 << 22) + 1) == 0
+    assert need(0, 5, 5) == need(500, 0, 5) == need(500, 5, 0) == need(1 << 31, 5, 5) == need(500, 5, (1 << 22) + 1) == 0
+    assert need(128, 5, 5) == 0 < need(129, 5, 5)
 
 
 def desc(b, **kw):
@@ -161,6 +162,8 @@ def test_binding_refuses_what_the_library_cannot_see(b, monkeypatch):
             return 0
     with pytest.raises(ValueError, match="current GPU"):
         b._current(Elsewhere())
+    with pytest.raises(ValueError, match="current GPU"):
+        b._ptrs(t)
     with pytest.raises(TypeError):
         b._index_ptr(torch.zeros(3, dtype=torch.int16))
     with pytest.raises(ValueError):
@@ -169,14 +172,18 @@ def test_binding_refuses_what_the_library_cannot_see(b, monkeypatch):
         b.cg_share_embedding_grad(t, t, ids, 4)                              # 4 rows of gradient for 3 ids
     with pytest.raises(ValueError):
         b.cg_share_embedding_grad(t[:3], t[:3], ids, 4, accumulate=True)     # nothing to add to
+    monkeypatch.setattr(b, "_device", lambda: -1)                            # where CPU tensors say they are
     x = torch.zeros((2, 3, 4), **i64)
     for bad in (x.transpose(0, 1), x[..., ::2], x.reshape(6, 4), x.int()):
         with pytest.raises((ValueError, TypeError)):
             b._head_rows(bad)
     with pytest.raises(ValueError):
-        b._head_pair(x, torch.zeros((2, 5, 4), **i64)[:, :3])                # rows not equally far apart
-    assert b._head_rows(torch.zeros((2, 5, 4), **i64)[:, 1:4])[1] == 20
-    assert b._head_rows(torch.zeros((1, 5, 4), **i64)[:, 1:4])[1] == 12      # one row: nothing to be apart from
+        b._head_rows(x, torch.zeros((2, 5, 4), **i64)[:, :3])                # rows not equally far apart
+    with pytest.raises(ValueError):
+        b._head_rows(x, x[:1])
+    assert b._head_rows(torch.zeros((2, 5, 4), **i64)[:, 1:4])[0] == 20
+    assert b._head_rows(torch.zeros((1, 5, 4), **i64)[:, 1:4])[0] == 12      # one row: nothing to be apart from
+    monkeypatch.setattr(b, "_device", lambda: 1)
     with pytest.raises(ValueError):
         b.ShareList([t], [t[:2]])
     with pytest.raises(ValueError):
