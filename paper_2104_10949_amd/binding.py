@@ -170,10 +170,12 @@ def _stream(stream) -> int:
 
 def _current(*tensors) -> None:
     """Calls launch on the current device: all their tensors have to live there."""
-    d = _device() if _device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+    d = tensors[0].get_device() if tensors else -1
     for t in tensors:
-        if t.get_device() != d:
-            raise ValueError(f"tensors must live on the current GPU ({d}), got one on {t.device}")
+        if t.get_device() != d or d < 0:
+            raise ValueError(f"tensors must live on the current GPU, got some on {tensors[0].device} and {t.device}")
+    if tensors and d != (_device() if _device is not None else torch.cuda.current_device()):
+        raise ValueError(f"tensors must live on the current GPU, got some on {tensors[0].device}")
 
 
 _INT64 = torch.int64
@@ -181,8 +183,12 @@ _INT64 = torch.int64
 
 def _ptrs(*tensors) -> list:
     """Addresses of contiguous ring tensors on the current device."""
-    _current(*tensors)
-    return [t.data_ptr() if t.dtype is _INT64 and t.is_contiguous() else _ptr(t) for t in tensors]
+    d = tensors[0].get_device()
+    out = [t.data_ptr() for t in tensors if t.dtype is _INT64 and t.get_device() == d and t.is_contiguous()]
+    if len(out) != len(tensors) or d < 0 or d != (_device() if _device is not None else torch.cuda.current_device()):
+        _current(*tensors)
+        out = [_ptr(t) for t in tensors]   # says which tensor and why
+    return out
 
 
 def _check(status: int, where: str) -> None:
@@ -656,8 +662,8 @@ def cg_share_col_sum(xa, xb, za=None, zb=None, stream=None):
 
 def _index_ptr(t: torch.Tensor) -> Tuple[int, int]:
     """Address and bytes per entry of a tensor of ids or positions."""
-    width = {torch.int64: 8, torch.int32: 4}.get(t.dtype)
-    if width is None:
+    width = 8 if t.dtype is _INT64 else 4
+    if width == 4 and t.dtype is not torch.int32:
         raise TypeError(f"ids and positions are torch.int64 or torch.int32, got {t.dtype}")
     _current(t)
     if not t.is_contiguous():
@@ -715,11 +721,8 @@ def cg_share_embedding_grad_workspace_bytes(n: int, V: int, D: int) -> int:
 def _head_rows(a: torch.Tensor, *others) -> Tuple[int, list]:
     """Words from a row to the next, and the addresses, of [rows, heads, dim] tensors whose rows are whole but may lie apart: the
     components of a pair, alike."""
-    _current(a, *others)
     shape, stride = a.shape, a.stride()
-    for t in (a, *others):
-        if t.dtype is not _INT64:
-            raise TypeError(f"ring tensors are torch.int64 (uint64 bit patterns), got {t.dtype}")
+    for t in others:
         if t.shape != shape:
             raise ValueError("heads must be [rows, heads, dim] tensors of one shape")
         if t.stride() != stride:
@@ -730,7 +733,12 @@ def _head_rows(a: torch.Tensor, *others) -> Tuple[int, list]:
     step, head, one = stride
     if (one != 1 and dim > 1) or (head != dim and heads > 1):
         raise ValueError("the heads of a row must lie next to each other")
-    return step if rows > 1 else heads * dim, [t.data_ptr() for t in (a, *others)]
+    tensors = (a, *others)
+    _current(*tensors)
+    for t in tensors:
+        if t.dtype is not _INT64:
+            raise TypeError(f"ring tensors are torch.int64 (uint64 bit patterns), got {t.dtype}")
+    return step if rows > 1 else heads * dim, [t.data_ptr() for t in tensors]
 
 
 def cg_share_head_sq_sum(x_i, x_ip1, z_i=None, stream=None) -> torch.Tensor:
@@ -755,7 +763,8 @@ def _head_desc(x_i, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, in
     if cos is None or sin is None or pos is None or cos.dim() != 2 or sin.shape != cos.shape or pos.shape != (rows,):
         raise ValueError("angles are a pair of [positions, rot / 2] tensors, with a position for each row")
     pp, width = _index_ptr(pos)
-    d = HeadDesc(rows, heads, dim, 2 * cos.shape[1], ld_x, ld_g, ld_out, cos.shape[0], width, frac_bits, bool(interleaved))
+    positions, half = cos.shape
+    d = HeadDesc(rows, heads, dim, 2 * half, ld_x, ld_g, ld_out, positions, width, frac_bits, bool(interleaved))
     return d, (*_ptrs(r_i, r_ip1, cos, sin), pp)
 
 

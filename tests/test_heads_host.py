@@ -172,7 +172,8 @@ def test_binding_refuses_what_the_library_cannot_see(b, monkeypatch):
         b.cg_share_embedding_grad(t, t, ids, 4)                              # 4 rows of gradient for 3 ids
     with pytest.raises(ValueError):
         b.cg_share_embedding_grad(t[:3], t[:3], ids, 4, accumulate=True)     # nothing to add to
-    monkeypatch.setattr(b, "_device", lambda: -1)                            # where CPU tensors say they are
+    real = b._current
+    monkeypatch.setattr(b, "_current", lambda *tensors: None)
     x = torch.zeros((2, 3, 4), **i64)
     for bad in (x.transpose(0, 1), x[..., ::2], x.reshape(6, 4), x.int()):
         with pytest.raises((ValueError, TypeError)):
@@ -183,7 +184,7 @@ def test_binding_refuses_what_the_library_cannot_see(b, monkeypatch):
         b._head_rows(x, x[:1])
     assert b._head_rows(torch.zeros((2, 5, 4), **i64)[:, 1:4])[0] == 20
     assert b._head_rows(torch.zeros((1, 5, 4), **i64)[:, 1:4])[0] == 12      # one row: nothing to be apart from
-    monkeypatch.setattr(b, "_device", lambda: 1)
+    monkeypatch.setattr(b, "_current", real)
     with pytest.raises(ValueError):
         b.ShareList([t], [t[:2]])
     with pytest.raises(ValueError):
