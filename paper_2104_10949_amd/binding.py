@@ -678,8 +678,8 @@ def cg_share_embedding(ta, tb, ids, alpha: int = 1, za=None, zb=None, stream=Non
         raise ValueError("the table must be a pair of [V, D] tensors")
     V, D = ta.shape
     shape = (*ids.shape, D)
-    za = torch.empty(shape, dtype=torch.int64, device=ta.device) if za is None else za
-    zb = torch.empty(shape, dtype=torch.int64, device=ta.device) if zb is None else zb
+    za = ta.new_empty(shape) if za is None else za
+    zb = ta.new_empty(shape) if zb is None else zb
     if za.shape != shape or zb.shape != shape:
         raise ValueError("output shape does not match")
     pta, ptb, pza, pzb = _ptrs(ta, tb, za, zb)
@@ -699,8 +699,8 @@ def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=Non
     D = ga.shape[-1]
     if accumulate and (da is None or db is None):
         raise ValueError("accumulate needs the tensors to add to")
-    da = torch.empty((V, D), dtype=torch.int64, device=ga.device) if da is None else da
-    db = torch.empty((V, D), dtype=torch.int64, device=ga.device) if db is None else db
+    da = ga.new_empty((V, D)) if da is None else da
+    db = ga.new_empty((V, D)) if db is None else db
     if da.shape != (V, D) or db.shape != (V, D):
         raise ValueError("output shape does not match")
     pga, pgb, pda, pdb = _ptrs(ga, gb, da, db)
@@ -718,54 +718,59 @@ def cg_share_embedding_grad_workspace_bytes(n: int, V: int, D: int) -> int:
     return int(lib().cg_share_embedding_grad_workspace_bytes(n, V, D))
 
 
-def _head_rows(a: torch.Tensor, *others) -> Tuple[int, list]:
-    """Words from a row to the next, and the addresses, of [rows, heads, dim] tensors whose rows are whole but may lie apart: the
-    components of a pair, alike."""
-    shape, stride = a.shape, a.stride()
-    for t in others:
-        if t.shape != shape:
-            raise ValueError("heads must be [rows, heads, dim] tensors of one shape")
-        if t.stride() != stride:
-            raise ValueError("both components must have their rows equally far apart")
-    if len(shape) != 3:
-        raise ValueError("heads must be [rows, heads, dim] tensors of one shape")
-    rows, heads, dim = shape
-    step, head, one = stride
+def _row_step(t: torch.Tensor) -> int:
+    """Words from a row to the next of a [rows, heads, dim] tensor whose rows are whole but may lie apart."""
+    rows, heads, dim = t.shape
+    step, head, one = t.stride()
     if (one != 1 and dim > 1) or (head != dim and heads > 1):
         raise ValueError("the heads of a row must lie next to each other")
-    tensors = (a, *others)
+    return step if rows > 1 else heads * dim
+
+
+def _pair_step(a: torch.Tensor, b: torch.Tensor, shape) -> int:
+    """... of both components."""
+    if a.shape != shape or b.shape != shape or len(shape) != 3:
+        raise ValueError("heads must be [rows, heads, dim] tensors of one shape")
+    if a.stride() != b.stride():
+        raise ValueError("both components must have their rows equally far apart")
+    return _row_step(a)
+
+
+def _ring_ptrs(*tensors) -> list:
+    """Addresses of ring tensors on the current device, whatever their strides."""
     _current(*tensors)
     for t in tensors:
         if t.dtype is not _INT64:
             raise TypeError(f"ring tensors are torch.int64 (uint64 bit patterns), got {t.dtype}")
-    return step if rows > 1 else heads * dim, [t.data_ptr() for t in tensors]
+    return [t.data_ptr() for t in tensors]
 
 
 def cg_share_head_sq_sum(x_i, x_ip1, z_i=None, stream=None) -> torch.Tensor:
     """z_i [rows, heads]: the party's additive share of each head's sum of squares; x [rows, heads, dim], a slice of wider rows
     (packed queries, keys and values) as it is."""
-    ld, px = _head_rows(x_i, x_ip1)
+    ld = _pair_step(x_i, x_ip1, x_i.shape)
     rows, heads, dim = x_i.shape
-    z_i = torch.empty((rows, heads), dtype=torch.int64, device=x_i.device) if z_i is None else z_i
-    if z_i.shape != (rows, heads):
-        raise ValueError("output shape does not match")
-    _check(lib().cg_share_head_sq_sum(*px, *_ptrs(z_i), rows, heads, dim, ld, _stream(stream)), "cg_share_head_sq_sum")
+    if z_i is None:
+        z_i = x_i.new_empty((rows, heads))
+    elif z_i.shape != (rows, heads) or not z_i.is_contiguous():
+        raise ValueError("the sums must be a contiguous [rows, heads] tensor")
+    _check(lib().cg_share_head_sq_sum(*_ring_ptrs(x_i, x_ip1, z_i), rows, heads, dim, ld, _stream(stream)), "cg_share_head_sq_sum")
     return z_i
 
 
-def _head_desc(x_i, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved):
+def _head_desc(shape, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved):
     """The descriptor, and the addresses of the shared norms, of the angles and of the positions."""
-    rows, heads, dim = x_i.shape
+    rows, heads, dim = shape
     if r_i.shape != (rows, heads) or r_ip1.shape != (rows, heads):
         raise ValueError("the norms must be a pair of [rows, heads] tensors")
     if cos is None and sin is None and pos is None:
-        return HeadDesc(rows, heads, dim, 0, ld_x, ld_g, ld_out, 0, 8, frac_bits, bool(interleaved)), (*_ptrs(r_i, r_ip1), 0, 0, 0)
+        return HeadDesc(rows, heads, dim, 0, ld_x, ld_g, ld_out, 0, 8, frac_bits, bool(interleaved)), _ptrs(r_i, r_ip1) + [0, 0, 0]
     if cos is None or sin is None or pos is None or cos.dim() != 2 or sin.shape != cos.shape or pos.shape != (rows,):
         raise ValueError("angles are a pair of [positions, rot / 2] tensors, with a position for each row")
     pp, width = _index_ptr(pos)
     positions, half = cos.shape
     d = HeadDesc(rows, heads, dim, 2 * half, ld_x, ld_g, ld_out, positions, width, frac_bits, bool(interleaved))
-    return d, (*_ptrs(r_i, r_ip1, cos, sin), pp)
+    return d, _ptrs(r_i, r_ip1, cos, sin) + [pp]
 
 
 def cg_share_head_norm_rotate(x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=None, frac_bits: int = 0, interleaved: bool = False,
@@ -773,13 +778,16 @@ def cg_share_head_norm_rotate(x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=No
     """z_i [rows, heads, dim]: three-term product of each head with its shared inverse norm r [rows, heads], the first
     rot = 2 * cos.shape[1] elements turned by the public angles of the row's position, the others times 2^frac_bits.  Without
     angles the product alone, times 2^frac_bits."""
-    ld_x, px = _head_rows(x_i, x_ip1)
-    z_i = torch.empty(x_i.shape, dtype=torch.int64, device=x_i.device) if z_i is None else z_i
-    ld_out, pz = _head_rows(z_i)
-    if z_i.shape != x_i.shape:
-        raise ValueError("output shape does not match")
-    d, rest = _head_desc(x_i, ld_x, 0, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved)
-    _check(lib().cg_share_head_norm_rotate(*px, *rest, *pz, ctypes.byref(d), _stream(stream)), "cg_share_head_norm_rotate")
+    shape = x_i.shape
+    ld_x = _pair_step(x_i, x_ip1, shape)
+    if z_i is None:
+        rows, heads, dim = shape
+        z_i, ld_out = x_i.new_empty((rows, heads, dim)), heads * dim
+    else:
+        ld_out = _pair_step(z_i, z_i, shape)
+    d, rest = _head_desc(shape, ld_x, 0, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved)
+    px, px1, pz = _ring_ptrs(x_i, x_ip1, z_i)
+    _check(lib().cg_share_head_norm_rotate(px, px1, *rest, pz, ctypes.byref(d), _stream(stream)), "cg_share_head_norm_rotate")
     return z_i
 
 
@@ -787,15 +795,20 @@ def cg_share_head_norm_rotate_grad(g_i, g_ip1, x_i, x_ip1, r_i, r_ip1, cos=None,
                                    interleaved: bool = False, dx_i=None, dr_i=None, stream=None):
     """(dx_i [rows, heads, dim], dr_i [rows, heads]): the party's additive shares of the gradients with respect to the heads and
     to their inverse norms, from the gradient pair g of cg_share_head_norm_rotate's result."""
-    ld_x, px = _head_rows(x_i, x_ip1)
-    ld_g, pg = _head_rows(g_i, g_ip1)
-    dx_i = torch.empty(x_i.shape, dtype=torch.int64, device=x_i.device) if dx_i is None else dx_i
-    dr_i = torch.empty(x_i.shape[:2], dtype=torch.int64, device=x_i.device) if dr_i is None else dr_i
-    ld_out, pd = _head_rows(dx_i)
-    if not (g_i.shape == x_i.shape == dx_i.shape) or dr_i.shape != x_i.shape[:2]:
-        raise ValueError("operand shapes do not match")
-    d, rest = _head_desc(x_i, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved)
-    _check(lib().cg_share_head_norm_rotate_grad(*pg, *px, *rest, *pd, *_ptrs(dr_i), ctypes.byref(d), _stream(stream)),
+    shape = x_i.shape
+    ld_x, ld_g = _pair_step(x_i, x_ip1, shape), _pair_step(g_i, g_ip1, shape)
+    rows, heads, dim = shape
+    if dx_i is None:
+        dx_i, ld_out = x_i.new_empty((rows, heads, dim)), heads * dim
+    else:
+        ld_out = _pair_step(dx_i, dx_i, shape)
+    if dr_i is None:
+        dr_i = x_i.new_empty((rows, heads))
+    elif dr_i.shape != (rows, heads) or not dr_i.is_contiguous():
+        raise ValueError("the norms' gradient must be a contiguous [rows, heads] tensor")
+    d, rest = _head_desc(shape, ld_x, ld_g, ld_out, r_i, r_ip1, cos, sin, pos, frac_bits, interleaved)
+    pg, pg1, px, px1, pdx, pdr = _ring_ptrs(g_i, g_ip1, x_i, x_ip1, dx_i, dr_i)
+    _check(lib().cg_share_head_norm_rotate_grad(pg, pg1, px, px1, *rest, pdx, pdr, ctypes.byref(d), _stream(stream)),
            "cg_share_head_norm_rotate_grad")
     return dx_i, dr_i
 
@@ -831,7 +844,7 @@ def cg_share_sq_norm(x: ShareList, z_i=None, stream=None) -> torch.Tensor:
 def cg_clip_factor(s0, s1, s2, max_norm: int, frac_bits: int, factor=None, stream=None) -> torch.Tensor:
     """factor [1]: 2^frac_bits, or that times max_norm / norm rounded down where the norm, the root of the opened sum s0 + s1 + s2
     of one word each, is larger; max_norm is a fixed-point word of the gradients' scale."""
-    factor = torch.empty((1,), dtype=torch.int64, device=s0.device) if factor is None else factor
+    factor = s0.new_empty((1,)) if factor is None else factor
     if any(t.numel() != 1 for t in (s0, s1, s2, factor)):
         raise ValueError("the shares of the squared norm and the factor are one word each")
     if not 0 <= int(max_norm) < 1 << 64:

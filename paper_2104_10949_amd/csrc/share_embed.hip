@@ -296,13 +296,13 @@ __global__ __launch_bounds__(THREADS) void group_list_kernel(const Id* __restric
     }
 }
 
-// Sum of the pieces of the rows list[0 .. count), loads of four rows under way at a time.  Lanes behind the row's end
-// read its last words and write nothing.
-template <int W>
+// Sum of the pieces of several rows, loads of R of them under way at a time.  Lanes behind the row's end read its last
+// words and write nothing.
+template <int W, int ACCESSES, int ROWS>
 struct RowSum {
     typedef typename Words<W>::type T;
-    static const int U = W == 2 ? 2 : 4;   // accesses per component and lane: 256 words a piece of a whole wave
-    static const int R = W == 2 ? 4 : 2;
+    static const int U = ACCESSES;   // per component and lane
+    static const int R = ROWS;
     T a[U], b[U];
 
     __device__ __forceinline__ void clear() {
@@ -310,12 +310,16 @@ struct RowSum {
         for (int u = 0; u < U; ++u) a[u] = b[u] = T(0);
     }
 
+    // the first `valid` of N rows; all loads are under way before the first sum
     template <int N>
     __device__ __forceinline__ void add(const u64* __restrict__ ga, const u64* __restrict__ gb, const unsigned (&row)[N],
-                                        u64 D, const u64 (&c)[U]) {
+                                        unsigned valid, u64 D, const u64 (&c)[U]) {
         T x[N][U], y[N][U];
 #pragma unroll
         for (int r = 0; r < N; ++r) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[r][u] = y[r][u] = T(0);
+            if (r > 0 && r >= (int)valid) continue;
             const T *pa = reinterpret_cast<const T*>(ga + row[r] * D), *pb = reinterpret_cast<const T*>(gb + row[r] * D);
 #pragma unroll
             for (int u = 0; u < U; ++u) { x[r][u] = __builtin_nontemporal_load(pa + c[u]); y[r][u] = __builtin_nontemporal_load(pb + c[u]); }
@@ -326,24 +330,25 @@ struct RowSum {
             for (int u = 0; u < U; ++u) { a[u] += x[r][u]; b[u] += y[r][u]; }
     }
 
-    // WAVE: the whole wave works on one row: its tokens are uniform and the addresses scalar (count <= 64)
-    template <bool WAVE>
-    __device__ __forceinline__ void gather(const u64* __restrict__ ga, const u64* __restrict__ gb,
-                                           const unsigned* __restrict__ list, unsigned count, u64 D, const u64 (&c)[U]) {
-        clear();
-        unsigned mine = 0;
-        const int lane = threadIdx.x & 63;
-        if (WAVE && lane < (int)count) mine = list[lane];
-        unsigned i = 0;
-        for (; i + R <= count; i += R) {
+    // the whole wave works on one row: token i of `count`, at most 64, is in lane i, and the addresses are scalar
+    __device__ __forceinline__ void add_tokens(const u64* __restrict__ ga, const u64* __restrict__ gb, unsigned mine,
+                                               unsigned count, u64 D, const u64 (&c)[U]) {
+        for (unsigned i = 0; i < count; i += R) {
             unsigned row[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) row[r] = WAVE ? __builtin_amdgcn_readlane(mine, i + r) : list[i + r];
-            add(ga, gb, row, D, c);
+            for (int r = 0; r < R; ++r) row[r] = __builtin_amdgcn_readlane(mine, i + r < count ? i + r : i);
+            add(ga, gb, row, count - i, D, c);
         }
-        for (; i < count; ++i) {
-            const unsigned row[1] = {WAVE ? (unsigned)__builtin_amdgcn_readlane(mine, i) : list[i]};
-            add(ga, gb, row, D, c);
+    }
+
+    // every lane goes through its own row's tokens
+    __device__ __forceinline__ void add_list(const u64* __restrict__ ga, const u64* __restrict__ gb,
+                                             const unsigned* __restrict__ list, unsigned count, u64 D, const u64 (&c)[U]) {
+        for (unsigned i = 0; i < count; i += R) {
+            unsigned row[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) row[r] = list[i + r < count ? i + r : i];
+            add(ga, gb, row, count - i, D, c);
         }
     }
 };
@@ -356,6 +361,9 @@ __device__ __forceinline__ void add_atomically(ull2* p, ull2 v) {
     add_atomically(reinterpret_cast<u64*>(p) + 1, v.y);
 }
 
+template <int W>
+using GroupSum = RowSum<W, W == 2 ? 2 : 4, W == 2 ? 4 : 2>;   // 256 words a piece of a whole wave
+
 const int FILL_ACCESSES = 8;   // accesses per lane and component of a wave that clears: 8 KB in a row
 
 // The items, by blocks below item_blocks, the pieces of a row next to each other so that its memory is read in one go; the
@@ -365,7 +373,7 @@ __global__ __launch_bounds__(THREADS) void group_sum_kernel(const u64* __restric
                                                             u64* da, u64* db, u64 V, u64 D, int accumulate, int lg,
                                                             unsigned pieces, unsigned item_blocks, Grouped g) {
     typedef typename Words<W>::type T;
-    const int U = RowSum<W>::U;
+    const int U = GroupSum<W>::U;
     const unsigned units = (unsigned)(D / W);
     if (blockIdx.x >= item_blocks) {
         const u64 all = V * units, chunk = FILL_ACCESSES * 64;
@@ -399,8 +407,14 @@ __global__ __launch_bounds__(THREADS) void group_sum_kernel(const u64* __restric
             if (c[u] >= units) c[u] = units - 1;
         }
         const Item it = g.items[index];
-        RowSum<W> sum;
-        sum.template gather<WAVE>(ga, gb, g.list + it.first, it.count, D, c);
+        GroupSum<W> sum;
+        sum.clear();
+        if (WAVE) {
+            const int lane = threadIdx.x & 63;
+            sum.add_tokens(ga, gb, lane < (int)it.count ? g.list[it.first + lane] : 0, it.count, D, c);
+        } else {
+            sum.add_list(ga, gb, g.list + it.first, it.count, D, c);
+        }
         T *pa = reinterpret_cast<T*>(da + it.row * D), *pb = reinterpret_cast<T*>(db + it.row * D);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -441,61 +455,52 @@ void launch_embed(const u64* ta, const u64* tb, const void* ids, u64 alpha, u64*
                        dim3(THREADS), 0, s, ta, tb, static_cast<const Id*>(ids), alpha, za, zb, n, V, D, lg);
 }
 
-// ---- gradient of a handful of tokens: one launch, no scratch memory ----
-// Every wave holds all ids, FEW / 64 per lane, and takes pieces of rows in turn: a ballot names the row's tokens.  Without
-// any the piece is a store of zeros.  Accumulating, the rows are those of the tokens instead, each by its first one.
-const u64 FEW = 128;
+// ---- gradient of few tokens: one launch, no scratch memory ----
+// Every block holds all ids in LDS, and its waves take pieces of rows in turn: ballots over the ids name the row's tokens.
+// Without any the piece is a store of zeros.  A piece of a row with more than OWN tokens waits until the block has come to its
+// end: then the waves share its tokens out and add up their sums in LDS (777 tokens of 1531 x 515, 73 of them the same: 19 us
+// in two launches by way of a list, 9 us this way).  Accumulating, the rows are those of the tokens, each by its first one.
+const int FEW = 1024, WAITING = 256, WAVES = THREADS / 64;
+// eight rows under way at a time: the kernel is made for calls in which the time of a round trip to memory counts
+template <int W>
+using FewSum = RowSum<W, 2, 8>;
+const int OWN = 8;
 
 template <class Id, int W>
 __global__ __launch_bounds__(THREADS) void few_sum_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
                                                           const Id* __restrict__ ids, u64 alpha, u64* da, u64* db, u64 n, u64 V,
-                                                          u64 D, int accumulate, unsigned pieces) {
+                                                          u64 D, int accumulate, unsigned pieces, unsigned pieces_each,
+                                                          unsigned shares) {
     typedef typename Words<W>::type T;
-    const int U = RowSum<W>::U, lane = threadIdx.x & 63;
-    const unsigned units = (unsigned)(D / W);
-    u64 id[FEW / 64];
-#pragma unroll
-    for (int k = 0; k < (int)(FEW / 64); ++k) {
-        const u64 j = lane + 64 * k;
-        id[k] = j < n ? (u64)(long long)ids[j] : ~(u64)0;
+    typedef FewSum<W> Sum;
+    const int U = Sum::U, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned units = (unsigned)(D / W), steps = (unsigned)(n + 63) / 64;
+    __shared__ unsigned key[FEW];
+    __shared__ u64 waiting[WAITING];
+    __shared__ unsigned waiting_count;
+    __shared__ T part[WAVES - 1][2 * U][64];
+    for (unsigned j = threadIdx.x; j < steps * 64; j += THREADS) {
+        const u64 id = j < n ? (u64)(long long)ids[j] : ~(u64)0;
+        key[j] = id < V ? (unsigned)id : EMPTY;
     }
-    const u64 all = (accumulate ? n : V) * pieces, step = (u64)gridDim.x * (THREADS / 64);
-    for (u64 q = (u64)blockIdx.x * (THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); q < all; q += step) {
-        u64 row = q / pieces;
-        const unsigned c0 = (unsigned)(q - row * pieces) * (U * 64) + lane, token = (unsigned)row;
-        if (accumulate) {
-            row = (u64)(long long)ids[token];
-            if (row >= V) continue;
-        }
-        u64 who[FEW / 64];
-        unsigned count = 0;
-#pragma unroll
-        for (int k = 0; k < (int)(FEW / 64); ++k) {
-            who[k] = __ballot(id[k] == row);
-            count += __popcll(who[k]);
-        }
-        if (accumulate && token != (who[0] ? (unsigned)__builtin_ctzll(who[0]) : 64 + (unsigned)__builtin_ctzll(who[1]))) continue;
-        u64 c[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) c[u] = c0 + u * 64 < units ? c0 + u * 64 : units - 1;
-        RowSum<W> sum;
-        sum.clear();
-        const auto next = [&]() {
-            const int k = who[0] ? 0 : 1;
-            const unsigned j = 64 * k + (unsigned)__builtin_ctzll(who[k]);
-            who[k] &= who[k] - 1;
-            return j;
-        };
-        for (; count >= RowSum<W>::R; count -= RowSum<W>::R) {
-            unsigned j[RowSum<W>::R];
-#pragma unroll
-            for (int r = 0; r < RowSum<W>::R; ++r) j[r] = next();
-            sum.add(ga, gb, j, D, c);
-        }
-        for (; count > 0; --count) {
-            const unsigned j[1] = {next()};
-            sum.add(ga, gb, j, D, c);
-        }
+    if (threadIdx.x == 0) waiting_count = 0;
+    __syncthreads();
+
+    // adds up the tokens of `row` among the ids of every `every`-th group of 64 from `from` on
+    const auto gather = [&](Sum& sum, unsigned row, unsigned from, unsigned every, const u64 (&c)[U]) {
+        unsigned mine = 0, count = 0;
+        for (unsigned k = from; k < steps; k += every)
+            for (u64 who = __ballot(key[64 * k + lane] == row); who; who &= who - 1) {
+                const unsigned j = 64 * k + (unsigned)__builtin_ctzll(who);
+                mine = lane == (int)count ? j : mine;
+                if (++count == 64) {
+                    sum.add_tokens(ga, gb, mine, 64, D, c);
+                    count = 0;
+                }
+            }
+        sum.add_tokens(ga, gb, mine, count, D, c);
+    };
+    const auto write = [&](const Sum& sum, unsigned row, unsigned c0, const u64 (&c)[U]) {
         T *pa = reinterpret_cast<T*>(da + row * D), *pb = reinterpret_cast<T*>(db + row * D);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -504,9 +509,85 @@ __global__ __launch_bounds__(THREADS) void few_sum_kernel(const u64* __restrict_
             if (accumulate) { pa[c[u]] += x; pb[c[u]] += y; }
             else { __builtin_nontemporal_store(x, pa + c[u]); __builtin_nontemporal_store(y, pb + c[u]); }
         }
+    };
+    const auto columns = [&](unsigned c0, u64 (&c)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) c[u] = c0 + u * 64 < units ? c0 + u * 64 : units - 1;
+    };
+
+    // a share is pieces_each pieces of a row
+    const u64 all = (accumulate ? n : V) * shares, step = (u64)gridDim.x * WAVES;
+    // (a block's waves take shares far apart: the frequent ids of a table are often neighbours)
+    for (u64 q = (u64)gridDim.x * wave + blockIdx.x; q < all; q += step) {
+        const u64 index = q / shares;
+        const unsigned piece0 = (unsigned)(q - index * shares) * pieces_each;
+        const unsigned row = accumulate ? key[index] : (unsigned)index;
+        if (row == EMPTY) continue;
+        unsigned count = 0, mine = 0;
+        for (unsigned k = 0; k < steps; ++k) {
+            u64 who = __ballot(key[64 * k + lane] == row);
+            for (; who && count < OWN; who &= who - 1, ++count) {
+                const unsigned j = 64 * k + (unsigned)__builtin_ctzll(who);
+                mine = lane == (int)count ? j : mine;
+            }
+            count += (unsigned)__popcll(who);
+        }
+        if (accumulate && (unsigned)__builtin_amdgcn_readfirstlane(mine) != (unsigned)index) continue;
+        bool own = count <= OWN;
+        if (!own) {
+            unsigned at = 0;
+            if (lane == 0) at = atomicAdd(&waiting_count, 1u);
+            at = __builtin_amdgcn_readfirstlane(at);
+            if (at < WAITING) {
+                if (lane == 0) waiting[at] = q;
+                continue;
+            }
+        }
+        for (unsigned piece = piece0; piece < piece0 + pieces_each && piece < pieces; ++piece) {
+            const unsigned c0 = piece * (U * 64) + lane;
+            u64 c[U];
+            columns(c0, c);
+            Sum sum;
+            sum.clear();
+            if (own) sum.add_tokens(ga, gb, mine, count, D, c);
+            else gather(sum, row, 0, 1, c);
+            write(sum, row, c0, c);
+        }
+    }
+    __syncthreads();
+    const unsigned many = waiting_count < WAITING ? waiting_count : WAITING;
+    for (unsigned i = 0; i < many; ++i) {
+        const u64 q = waiting[i], index = q / shares;
+        const unsigned piece0 = (unsigned)(q - index * shares) * pieces_each;
+        const unsigned row = accumulate ? key[index] : (unsigned)index;
+        for (unsigned piece = piece0; piece < piece0 + pieces_each && piece < pieces; ++piece) {
+            const unsigned c0 = piece * (U * 64) + lane;
+            u64 c[U];
+            columns(c0, c);
+            Sum sum;
+            sum.clear();
+            gather(sum, row, wave, WAVES, c);
+            if (wave > 0) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    part[wave - 1][u][lane] = sum.a[u];
+                    part[wave - 1][U + u][lane] = sum.b[u];
+                }
+            }
+            __syncthreads();
+            if (wave == 0) {
+                for (int w = 0; w < WAVES - 1; ++w)
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        sum.a[u] += part[w][u][lane];
+                        sum.b[u] += part[w][U + u][lane];
+                    }
+                write(sum, row, c0, c);
+            }
+            __syncthreads();
+        }
     }
 }
-static_assert(FEW == 128, "two ballots");
 
 struct GradCall {
     const u64 *ga, *gb;
@@ -521,7 +602,7 @@ unsigned blocks_of(u64 threads) { return (unsigned)((threads + THREADS - 1) / TH
 
 template <int W>
 void launch_sum(const GradCall& c, const Grouped& g, hipStream_t s) {
-    const int U = RowSum<W>::U;
+    const int U = GroupSum<W>::U;
     const u64 units = c.D / W;
     const int lg = row_lanes_log2((units + U - 1) / U);
     const u64 piece = (u64)U << lg, pieces = (units + piece - 1) / piece, per_fill = (u64)FILL_ACCESSES * THREADS;
@@ -539,11 +620,14 @@ void launch_sum(const GradCall& c, const Grouped& g, hipStream_t s) {
 
 template <class Id, int W>
 void launch_few(const GradCall& c, hipStream_t s) {
-    const u64 piece = RowSum<W>::U * 64, pieces = (c.D / W + piece - 1) / piece;
-    const u64 waves = (c.accumulate ? c.n : c.V) * pieces;
-    const unsigned blocks = (unsigned)(waves < 4 * 2048 ? (waves + 3) / 4 : 2048);
+    const u64 piece = FewSum<W>::U * 64, pieces = (c.D / W + piece - 1) / piece, rows = c.accumulate ? c.n : c.V;
+    // a wave looks through the ids once for all pieces of its share of a row: as many as leave 8192 waves something to do
+    u64 each = rows * pieces / 8192;
+    each = each < 1 ? 1 : each < pieces ? each : pieces;
+    const u64 shares = (pieces + each - 1) / each, waves = rows * shares;
+    const unsigned blocks = (unsigned)(waves < WAVES * 2048 ? (waves + WAVES - 1) / WAVES : 2048);
     hipLaunchKernelGGL((few_sum_kernel<Id, W>), dim3(blocks), dim3(THREADS), 0, s, c.ga, c.gb, static_cast<const Id*>(c.ids), c.alpha, c.da, c.db,
-                       c.n, c.V, c.D, c.accumulate, (unsigned)pieces);
+                       c.n, c.V, c.D, c.accumulate, (unsigned)pieces, (unsigned)each, (unsigned)shares);
 }
 
 template <class Id>
@@ -599,7 +683,7 @@ cg_status cg_share_embedding(const uint64_t* ta, const uint64_t* tb, const void*
 
 size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D) {
     int id = 0;
-    if (n <= FEW || check_sizes(&id, 4, n, V, D)) return 0;
+    if (n <= (size_t)FEW || check_sizes(&id, 4, n, V, D)) return 0;
     return (size_t)grouped_layout(reinterpret_cast<char*>(256), n, V).bytes;
 }
 
@@ -631,7 +715,7 @@ cg_status cg_share_embedding_grad(const uint64_t* ga, const uint64_t* gb, const 
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
     const GradCall c = {ga, gb, ids, alpha, da, db, n, V, D, accumulate};
-    if (n > 0 && n <= FEW) {
+    if (n > 0 && n <= (size_t)FEW) {
         if (id_bytes == 8) {
             if (vec) launch_few<long long, 2>(c, s);
             else launch_few<long long, 1>(c, s);

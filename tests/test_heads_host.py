@@ -62,8 +62,8 @@ def test_embedding_gradient_validation(b):
     assert need(n, V, D) > 8 * n
     for where in (P, 2 * P + n * D * 8 - 16, 3 * P + 16, 4 * P, 5 * P - need(n, V, D) + 16):
         assert call(n=n, V=V, D=D, ws=where, bytes=need(n, V, D)) == b.CG_ERR_ALIAS
-    assert need(0, 5, 5) == need(500, 0, 5) == need(500, 5, 0) == need(1 << 31, 5, 5) == need(500, 5, (1 << 22) + 1) == 0
-    assert need(128, 5, 5) == 0 < need(129, 5, 5)
+    assert need(0, 5, 5) == need(5000, 0, 5) == need(5000, 5, 0) == need(1 << 31, 5, 5) == need(5000, 5, (1 << 22) + 1) == 0
+    assert need(1024, 5, 5) == 0 < need(1025, 5, 5)
 
 
 def desc(b, **kw):
@@ -172,19 +172,19 @@ def test_binding_refuses_what_the_library_cannot_see(b, monkeypatch):
         b.cg_share_embedding_grad(t, t, ids, 4)                              # 4 rows of gradient for 3 ids
     with pytest.raises(ValueError):
         b.cg_share_embedding_grad(t[:3], t[:3], ids, 4, accumulate=True)     # nothing to add to
-    real = b._current
-    monkeypatch.setattr(b, "_current", lambda *tensors: None)
     x = torch.zeros((2, 3, 4), **i64)
-    for bad in (x.transpose(0, 1), x[..., ::2], x.reshape(6, 4), x.int()):
-        with pytest.raises((ValueError, TypeError)):
-            b._head_rows(bad)
+    with pytest.raises(TypeError):
+        monkeypatch.setattr(b, "_current", lambda *tensors: None)
+        b._ring_ptrs(x, x.int())
+    for bad in (x.transpose(0, 1), x[..., ::2], x.reshape(6, 4)):
+        with pytest.raises(ValueError):
+            b._pair_step(bad, bad, bad.shape)
     with pytest.raises(ValueError):
-        b._head_rows(x, torch.zeros((2, 5, 4), **i64)[:, :3])                # rows not equally far apart
+        b._pair_step(x, torch.zeros((2, 5, 4), **i64)[:, :3], x.shape)       # rows not equally far apart
     with pytest.raises(ValueError):
-        b._head_rows(x, x[:1])
-    assert b._head_rows(torch.zeros((2, 5, 4), **i64)[:, 1:4])[0] == 20
-    assert b._head_rows(torch.zeros((1, 5, 4), **i64)[:, 1:4])[0] == 12      # one row: nothing to be apart from
-    monkeypatch.setattr(b, "_current", real)
+        b._pair_step(x, x[:1], x.shape)
+    assert b._row_step(torch.zeros((2, 5, 4), **i64)[:, 1:4]) == 20
+    assert b._row_step(torch.zeros((1, 5, 4), **i64)[:, 1:4]) == 12          # one row: nothing to be apart from
     with pytest.raises(ValueError):
         b.ShareList([t], [t[:2]])
     with pytest.raises(ValueError):
