@@ -366,6 +366,26 @@ using GroupSum = RowSum<W, W == 2 ? 2 : 4, W == 2 ? 4 : 2>;   // 256 words a pie
 
 const int FILL_ACCESSES = 8;   // accesses per lane and component of a wave that clears: 8 KB in a row
 
+// Clears the rows of a table for which `empty` holds, in the order of the addresses: this block's part of `blocks` blocks'.
+template <int W, class Empty>
+__device__ __forceinline__ void clear_rows(u64* da, u64* db, u64 V, unsigned units, unsigned block, unsigned blocks, const Empty& empty) {
+    typedef typename Words<W>::type T;
+    const u64 all = V * units, chunk = FILL_ACCESSES * 64, waves = blockDim.x / 64;
+    T *pa = reinterpret_cast<T*>(da), *pb = reinterpret_cast<T*>(db);
+    for (u64 i0 = (block * waves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * chunk; i0 < all; i0 += blocks * waves * chunk) {
+        const u64 row0 = i0 / units;
+        const unsigned c0 = (unsigned)(i0 - row0 * units);
+#pragma unroll
+        for (int k = 0; k < FILL_ACCESSES; ++k) {
+            const unsigned off = k * 64 + (threadIdx.x & 63);
+            if (i0 + off < all && empty(row0 + (c0 + off) / units)) {
+                __builtin_nontemporal_store(T(0), pa + i0 + off);
+                __builtin_nontemporal_store(T(0), pb + i0 + off);
+            }
+        }
+    }
+}
+
 // The items, by blocks below item_blocks, the pieces of a row next to each other so that its memory is read in one go; the
 // other blocks clear the rows without tokens, in the order of the addresses.
 template <int W, bool WAVE>
@@ -376,22 +396,7 @@ __global__ __launch_bounds__(THREADS) void group_sum_kernel(const u64* __restric
     const int U = GroupSum<W>::U;
     const unsigned units = (unsigned)(D / W);
     if (blockIdx.x >= item_blocks) {
-        const u64 all = V * units, chunk = FILL_ACCESSES * 64;
-        const u64 step = (u64)(gridDim.x - item_blocks) * (THREADS / 64) * chunk;
-        T *pa = reinterpret_cast<T*>(da), *pb = reinterpret_cast<T*>(db);
-        for (u64 i0 = ((u64)(blockIdx.x - item_blocks) * (THREADS / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * chunk; i0 < all;
-             i0 += step) {
-            const u64 row0 = i0 / units;
-            const unsigned c0 = (unsigned)(i0 - row0 * units);
-#pragma unroll
-            for (int k = 0; k < FILL_ACCESSES; ++k) {
-                const unsigned off = k * 64 + (threadIdx.x & 63);
-                if (i0 + off < all && g.count[row0 + (c0 + off) / units] == 0) {
-                    __builtin_nontemporal_store(T(0), pa + i0 + off);
-                    __builtin_nontemporal_store(T(0), pb + i0 + off);
-                }
-            }
-        }
+        clear_rows<W>(da, db, V, units, blockIdx.x - item_blocks, gridDim.x - item_blocks, [&](u64 row) { return g.count[row] == 0; });
         return;
     }
     const unsigned used = (unsigned)(*g.cursor >> 32);
@@ -456,50 +461,53 @@ void launch_embed(const u64* ta, const u64* tb, const void* ids, u64 alpha, u64*
 }
 
 // ---- gradient of few tokens: one launch, no scratch memory ----
-// Every block holds all ids in LDS, and its waves take pieces of rows in turn: ballots over the ids name the row's tokens.
-// Without any the piece is a store of zeros.  A piece of a row with more than OWN tokens waits until the block has come to its
-// end: then the waves share its tokens out and add up their sums in LDS (777 tokens of 1531 x 515, 73 of them the same: 19 us
-// in two launches by way of a list, 9 us this way).  Accumulating, the rows are those of the tokens, each by its first one.
-const int FEW = 1024, WAITING = 256, WAVES = THREADS / 64;
-// eight rows under way at a time: the kernel is made for calls in which the time of a round trip to memory counts
+// The first blocks hold all ids in LDS, and each of their waves has a token and a share of its row: ballots over the ids name
+// the tokens of the same row, and the first of them adds them all up.  A row with more than OWN tokens waits until the
+// block has come to its end: then the waves share its tokens out and meet in LDS (777 tokens of 1531 x 515, 73 of them the same:
+// 19 us in two launches by way of a list, 14 us this way).  The other blocks clear the rows without tokens, which they know
+// from one bit per row in LDS.
+const int FEW = 1024, FEW_THREADS = 512, WAVES = FEW_THREADS / 64;
+const int FEW_ROWS = 1 << 18;
+// Sixteen rows under way at a time and pieces of one access per lane: what counts in these calls is the time of a round trip to
+// memory, and that a row of very many tokens is shared out over many compute units (1000 tokens of 768 words, all the same: 82 us with
+// eight rows and two accesses, 44 us this way; all different: 11 and 15 us).
 template <int W>
-using FewSum = RowSum<W, 2, 8>;
+using FewSum = RowSum<W, 1, 16>;
 const int OWN = 8;
 
 template <class Id, int W>
-__global__ __launch_bounds__(THREADS) void few_sum_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
-                                                          const Id* __restrict__ ids, u64 alpha, u64* da, u64* db, u64 n, u64 V,
-                                                          u64 D, int accumulate, unsigned pieces, unsigned pieces_each,
-                                                          unsigned shares) {
+__global__ __launch_bounds__(FEW_THREADS) void few_sum_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
+                                                              const Id* __restrict__ ids, u64 alpha, u64* da, u64* db, unsigned n,
+                                                              u64 V, u64 D, int accumulate, unsigned pieces, unsigned pieces_each,
+                                                              unsigned shares, unsigned sum_blocks) {
     typedef typename Words<W>::type T;
     typedef FewSum<W> Sum;
     const int U = Sum::U, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned units = (unsigned)(D / W), steps = (unsigned)(n + 63) / 64;
-    __shared__ unsigned key[FEW];
-    __shared__ u64 waiting[WAITING];
-    __shared__ unsigned waiting_count;
-    __shared__ T part[WAVES - 1][2 * U][64];
-    for (unsigned j = threadIdx.x; j < steps * 64; j += THREADS) {
+    const unsigned units = (unsigned)(D / W), steps = (n + 63) / 64;
+    __shared__ unsigned key[FEW], waiting[WAVES], waiting_count;
+    __shared__ union {
+        unsigned touched[FEW_ROWS / 32];
+        T part[WAVES - 1][2 * U][64];
+    } lds;
+    if (blockIdx.x >= sum_blocks) {
+        for (unsigned i = threadIdx.x; i < (V + 31) / 32; i += FEW_THREADS) lds.touched[i] = 0;
+        __syncthreads();
+        for (unsigned j = threadIdx.x; j < n; j += FEW_THREADS) {
+            const u64 id = (u64)(long long)ids[j];
+            if (id < V) atomicOr(&lds.touched[id >> 5], 1u << (id & 31));
+        }
+        __syncthreads();
+        clear_rows<W>(da, db, V, units, blockIdx.x - sum_blocks, gridDim.x - sum_blocks,
+                      [&](u64 row) { return !(lds.touched[row >> 5] >> (row & 31) & 1); });
+        return;
+    }
+    for (unsigned j = threadIdx.x; j < steps * 64; j += FEW_THREADS) {
         const u64 id = j < n ? (u64)(long long)ids[j] : ~(u64)0;
         key[j] = id < V ? (unsigned)id : EMPTY;
     }
     if (threadIdx.x == 0) waiting_count = 0;
     __syncthreads();
 
-    // adds up the tokens of `row` among the ids of every `every`-th group of 64 from `from` on
-    const auto gather = [&](Sum& sum, unsigned row, unsigned from, unsigned every, const u64 (&c)[U]) {
-        unsigned mine = 0, count = 0;
-        for (unsigned k = from; k < steps; k += every)
-            for (u64 who = __ballot(key[64 * k + lane] == row); who; who &= who - 1) {
-                const unsigned j = 64 * k + (unsigned)__builtin_ctzll(who);
-                mine = lane == (int)count ? j : mine;
-                if (++count == 64) {
-                    sum.add_tokens(ga, gb, mine, 64, D, c);
-                    count = 0;
-                }
-            }
-        sum.add_tokens(ga, gb, mine, count, D, c);
-    };
     const auto write = [&](const Sum& sum, unsigned row, unsigned c0, const u64 (&c)[U]) {
         T *pa = reinterpret_cast<T*>(da + row * D), *pb = reinterpret_cast<T*>(db + row * D);
 #pragma unroll
@@ -515,14 +523,11 @@ __global__ __launch_bounds__(THREADS) void few_sum_kernel(const u64* __restrict_
         for (int u = 0; u < U; ++u) c[u] = c0 + u * 64 < units ? c0 + u * 64 : units - 1;
     };
 
-    // a share is pieces_each pieces of a row
-    const u64 all = (accumulate ? n : V) * shares, step = (u64)gridDim.x * WAVES;
-    // (a block's waves take shares far apart: the frequent ids of a table are often neighbours)
-    for (u64 q = (u64)gridDim.x * wave + blockIdx.x; q < all; q += step) {
-        const u64 index = q / shares;
-        const unsigned piece0 = (unsigned)(q - index * shares) * pieces_each;
-        const unsigned row = accumulate ? key[index] : (unsigned)index;
-        if (row == EMPTY) continue;
+    // a share is pieces_each pieces of a token's row; a block's waves take shares far apart: the same id is often that of
+    // tokens close by, and its waves would wait for each other
+    const unsigned own_share = sum_blocks * wave + blockIdx.x, own_token = own_share / shares;
+    if (own_token < n && key[own_token] != EMPTY) {
+        const unsigned row = key[own_token];
         unsigned count = 0, mine = 0;
         for (unsigned k = 0; k < steps; ++k) {
             u64 who = __ballot(key[64 * k + lane] == row);
@@ -532,46 +537,49 @@ __global__ __launch_bounds__(THREADS) void few_sum_kernel(const u64* __restrict_
             }
             count += (unsigned)__popcll(who);
         }
-        if (accumulate && (unsigned)__builtin_amdgcn_readfirstlane(mine) != (unsigned)index) continue;
-        bool own = count <= OWN;
-        if (!own) {
-            unsigned at = 0;
-            if (lane == 0) at = atomicAdd(&waiting_count, 1u);
-            at = __builtin_amdgcn_readfirstlane(at);
-            if (at < WAITING) {
-                if (lane == 0) waiting[at] = q;
-                continue;
+        if ((unsigned)__builtin_amdgcn_readfirstlane(mine) != own_token) {
+            // another token is the first of this row
+        } else if (count > OWN) {
+            if (lane == 0) waiting[atomicAdd(&waiting_count, 1u)] = own_share;
+        } else {
+            const unsigned piece0 = (own_share - own_token * shares) * pieces_each;
+            for (unsigned piece = piece0; piece < piece0 + pieces_each && piece < pieces; ++piece) {
+                const unsigned c0 = piece * (U * 64) + lane;
+                u64 c[U];
+                columns(c0, c);
+                Sum sum;
+                sum.clear();
+                sum.add_tokens(ga, gb, mine, count, D, c);
+                write(sum, row, c0, c);
             }
-        }
-        for (unsigned piece = piece0; piece < piece0 + pieces_each && piece < pieces; ++piece) {
-            const unsigned c0 = piece * (U * 64) + lane;
-            u64 c[U];
-            columns(c0, c);
-            Sum sum;
-            sum.clear();
-            if (own) sum.add_tokens(ga, gb, mine, count, D, c);
-            else gather(sum, row, 0, 1, c);
-            write(sum, row, c0, c);
         }
     }
     __syncthreads();
-    const unsigned many = waiting_count < WAITING ? waiting_count : WAITING;
+    const unsigned many = waiting_count;
     for (unsigned i = 0; i < many; ++i) {
-        const u64 q = waiting[i], index = q / shares;
-        const unsigned piece0 = (unsigned)(q - index * shares) * pieces_each;
-        const unsigned row = accumulate ? key[index] : (unsigned)index;
+        const unsigned share = waiting[i], token = share / shares, piece0 = (share - token * shares) * pieces_each, row = key[token];
         for (unsigned piece = piece0; piece < piece0 + pieces_each && piece < pieces; ++piece) {
             const unsigned c0 = piece * (U * 64) + lane;
             u64 c[U];
             columns(c0, c);
             Sum sum;
             sum.clear();
-            gather(sum, row, wave, WAVES, c);
+            unsigned mine = 0, count = 0;
+            for (unsigned k = wave; k < steps; k += WAVES)   // every WAVES-th group of 64 ids is this wave's
+                for (u64 who = __ballot(key[64 * k + lane] == row); who; who &= who - 1) {
+                    const unsigned j = 64 * k + (unsigned)__builtin_ctzll(who);
+                    mine = lane == (int)count ? j : mine;
+                    if (++count == 64) {
+                        sum.add_tokens(ga, gb, mine, 64, D, c);
+                        count = 0;
+                    }
+                }
+            sum.add_tokens(ga, gb, mine, count, D, c);
             if (wave > 0) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    part[wave - 1][u][lane] = sum.a[u];
-                    part[wave - 1][U + u][lane] = sum.b[u];
+                    lds.part[wave - 1][u][lane] = sum.a[u];
+                    lds.part[wave - 1][U + u][lane] = sum.b[u];
                 }
             }
             __syncthreads();
@@ -579,8 +587,8 @@ __global__ __launch_bounds__(THREADS) void few_sum_kernel(const u64* __restrict_
                 for (int w = 0; w < WAVES - 1; ++w)
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        sum.a[u] += part[w][u][lane];
-                        sum.b[u] += part[w][U + u][lane];
+                        sum.a[u] += lds.part[w][u][lane];
+                        sum.b[u] += lds.part[w][U + u][lane];
                     }
                 write(sum, row, c0, c);
             }
@@ -618,16 +626,20 @@ void launch_sum(const GradCall& c, const Grouped& g, hipStream_t s) {
                            (unsigned)pieces, (unsigned)items, g);
 }
 
+// One launch without scratch memory: where the ids, and a bit per row that may have to be cleared, fit the LDS.
+bool few(u64 n, u64 V, int accumulate) { return n <= (u64)FEW && (accumulate || V <= (u64)FEW_ROWS); }
+
 template <class Id, int W>
 void launch_few(const GradCall& c, hipStream_t s) {
-    const u64 piece = FewSum<W>::U * 64, pieces = (c.D / W + piece - 1) / piece, rows = c.accumulate ? c.n : c.V;
+    const u64 units = c.D / W, piece = FewSum<W>::U * 64, pieces = (units + piece - 1) / piece;
     // a wave looks through the ids once for all pieces of its share of a row: as many as leave 8192 waves something to do
-    u64 each = rows * pieces / 8192;
+    u64 each = c.n * pieces / 8192;
     each = each < 1 ? 1 : each < pieces ? each : pieces;
-    const u64 shares = (pieces + each - 1) / each, waves = rows * shares;
-    const unsigned blocks = (unsigned)(waves < WAVES * 2048 ? (waves + WAVES - 1) / WAVES : 2048);
-    hipLaunchKernelGGL((few_sum_kernel<Id, W>), dim3(blocks), dim3(THREADS), 0, s, c.ga, c.gb, static_cast<const Id*>(c.ids), c.alpha, c.da, c.db,
-                       c.n, c.V, c.D, c.accumulate, (unsigned)pieces, (unsigned)each, (unsigned)shares);
+    const u64 shares = (pieces + each - 1) / each, sums = (c.n * shares + WAVES - 1) / WAVES, per_fill = (u64)FILL_ACCESSES * FEW_THREADS;
+    u64 fills = c.accumulate ? 0 : (c.V * units + per_fill - 1) / per_fill;
+    if (fills > 2048) fills = 2048;
+    hipLaunchKernelGGL((few_sum_kernel<Id, W>), dim3((unsigned)(sums + fills)), dim3(FEW_THREADS), 0, s, c.ga, c.gb, static_cast<const Id*>(c.ids),
+                       c.alpha, c.da, c.db, (unsigned)c.n, c.V, c.D, c.accumulate, (unsigned)pieces, (unsigned)each, (unsigned)shares, (unsigned)sums);
 }
 
 template <class Id>
@@ -683,7 +695,7 @@ cg_status cg_share_embedding(const uint64_t* ta, const uint64_t* tb, const void*
 
 size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D) {
     int id = 0;
-    if (n <= (size_t)FEW || check_sizes(&id, 4, n, V, D)) return 0;
+    if (check_sizes(&id, 4, n, V, D) || few(n, V, 0)) return 0;
     return (size_t)grouped_layout(reinterpret_cast<char*>(256), n, V).bytes;
 }
 
@@ -715,7 +727,7 @@ cg_status cg_share_embedding_grad(const uint64_t* ga, const uint64_t* gb, const 
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
     const GradCall c = {ga, gb, ids, alpha, da, db, n, V, D, accumulate};
-    if (n > 0 && n <= (size_t)FEW) {
+    if (n > 0 && few(n, V, accumulate)) {
         if (id_bytes == 8) {
             if (vec) launch_few<long long, 2>(c, s);
             else launch_few<long long, 1>(c, s);

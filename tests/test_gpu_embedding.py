@@ -118,7 +118,7 @@ def test_lookup_beyond_32_bit_offsets(cg):
 
 
 # (n, V, D): one token to many, rows shorter and longer than a wave's piece, tables smaller and larger than the batch
-GRADS = [(1, 1, 1), (1, 700, 512), (2, 5, 3), (63, 7, 16), (64, 64, 64), (65, 1000, 30), (128, 300, 514), (129, 300, 514), (100, 40, 1031), (500, 3, 515), (777, 1531, 130), (1024, 2000, 257), (1025, 100, 260), (1024, 3, 70000), (2048, 100, 258),
+GRADS = [(1, 1, 1), (1, 700, 512), (2, 5, 3), (63, 7, 16), (64, 64, 64), (65, 1000, 30), (128, 300, 514), (129, 300, 514), (100, 40, 1031), (500, 3, 515), (777, 1531, 130), (1024, 2000, 257), (1025, 100, 260), (1024, 3, 70000), (600, (1 << 18) + 5, 4), (600, 1 << 18, 4), (2048, 100, 258),
          (4096, 300, 8), (4097, 40, 64), (5000, 5000, 20), (3000, 9, 1030), (9001, 2000, 33), (20000, 700, 34), (16384, 16384, 6), (40000, 50, 18)]
 
 
