@@ -101,9 +101,14 @@ struct Item {
     unsigned row, first, count, whole;   // whole: all of the row's tokens
 };
 
+struct Frequent {   // a row of several items, not yet written down
+    unsigned row, first, count, slot;
+};
+
 struct Grouped {   // in the scratch memory
-    unsigned long long* cursor;   // tokens placed so far, and items in the upper half; starts at zero as the counts do
-    unsigned *count, *offset, *rank, *list;
+    unsigned long long* cursor;   // tokens placed so far, and items in the upper half; starts at zero, as frequent_used and the counts do
+    unsigned *frequent_used, *count, *offset, *rank, *list;
+    Frequent* frequent;
     Item* items;
     u64 items_max, bytes;
     unsigned most;      // tokens of an item, at most 64
@@ -114,18 +119,22 @@ const int GROUP_THREADS = 1024, GROUP_TOKENS = 4;   // of a block that groups, a
 const int TABLE = 2 * GROUP_THREADS * GROUP_TOKENS; // places of its hash table: at most half full
 const unsigned EMPTY = ~0u;                         // no row: V < 2^31
 
-Grouped grouped_layout(char* p, u64 n, u64 V) {
+Grouped grouped_layout(char* p, u64 n, u64 V, u64 D) {
     Grouped g = {};
-    // a wave takes about a microsecond for four tokens: items short enough not to outlast a small call, and in a large one
-    // few enough atomics
-    g.most = n < 8 * 256 ? 8 : n < 64 * 256 ? (unsigned)(n / 256) : 64;
+    // a wave takes two microseconds for four tokens: items short enough for 8192 waves of 256 words, and in a large call
+    // long enough to need few atomics (63904 tokens of 320 x 105: 53 us with 4 tokens, 36 with 8, 29 with 16, 58 with 64)
     g.one_block = n <= GROUP_THREADS * GROUP_TOKENS;
+    const unsigned least = g.one_block ? 8 : 16;
+    const double most = (double)n * (double)D / (256.0 * 8192.0);
+    g.most = most < least ? least : most < 64 ? (unsigned)most : 64;
     g.items_max = (n < V ? n : V) + 2 * n / g.most;   // rows with tokens; of those with c > most, ceil(c / most) items each
     u64 at = 0;
     const auto take = [&](u64 bytes) { char* q = p + at; at += (bytes + 255) / 256 * 256; return q; };
-    g.cursor = reinterpret_cast<unsigned long long*>(take(8 + (g.one_block ? 0 : V * 4)));
-    g.count = reinterpret_cast<unsigned*>(g.cursor + 1);
+    g.cursor = reinterpret_cast<unsigned long long*>(take(12 + (g.one_block ? 0 : V * 4)));
+    g.frequent_used = reinterpret_cast<unsigned*>(g.cursor + 1);
+    g.count = g.frequent_used + 1;
     if (!g.one_block) {
+        g.frequent = reinterpret_cast<Frequent*>(take(n / g.most * sizeof(Frequent)));
         g.offset = reinterpret_cast<unsigned*>(take(V * 4));
         g.rank = reinterpret_cast<unsigned*>(take(n * 4));
     }
@@ -271,13 +280,15 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_offset_kernel(u64 V, Grou
     __syncthreads();
     at += base;
     if (v < V) g.offset[v] = (unsigned)at;
-    write_items(g.items + (at >> 32), (unsigned)v, (unsigned)at, c, g.most);
+    if (c > g.most) g.frequent[atomicAdd(g.frequent_used, 1u)] = {(unsigned)v, (unsigned)at, c, (unsigned)(at >> 32)};
+    else write_items(g.items + (at >> 32), (unsigned)v, (unsigned)at, c, g.most);
 }
 
-// The first token_blocks blocks fill the list; the others clear the rows that items will be added to.
+// The first token_blocks blocks fill the list; the others write down the items of frequent rows and clear the rows that those
+// will be added to.
 template <class Id>
 __global__ __launch_bounds__(THREADS) void group_list_kernel(const Id* __restrict__ ids, u64 n, u64 V, u64 D, Grouped g,
-                                                             unsigned token_blocks, u64* da, u64* db) {
+                                                             unsigned token_blocks, int accumulate, u64* da, u64* db) {
     if (blockIdx.x < token_blocks) {
         const u64 j = (u64)blockIdx.x * THREADS + threadIdx.x;
         if (j >= n) return;
@@ -285,13 +296,17 @@ __global__ __launch_bounds__(THREADS) void group_list_kernel(const Id* __restric
         if (id < V) g.list[g.offset[id] + g.rank[j]] = (unsigned)j;
         return;
     }
-    const unsigned used = (unsigned)(*g.cursor >> 32);
-    for (unsigned k = blockIdx.x - token_blocks; k < used; k += gridDim.x - token_blocks) {
-        const Item it = g.items[k];
-        if (it.whole || it.first != g.offset[it.row]) continue;   // the first item of a row that has several
+    const unsigned used = *g.frequent_used;
+    for (unsigned i = blockIdx.x - token_blocks; i < used; i += gridDim.x - token_blocks) {
+        const Frequent f = g.frequent[i];
+        for (unsigned k = threadIdx.x; k * g.most < f.count; k += THREADS) {
+            const unsigned left = f.count - k * g.most;
+            g.items[f.slot + k] = {f.row, f.first + k * g.most, left < g.most ? left : g.most, 0};
+        }
+        if (accumulate) continue;
         for (u64 c = threadIdx.x; c < D; c += THREADS) {
-            da[it.row * D + c] = 0;
-            db[it.row * D + c] = 0;
+            da[f.row * D + c] = 0;
+            db[f.row * D + c] = 0;
         }
     }
 }
@@ -362,7 +377,7 @@ __device__ __forceinline__ void add_atomically(ull2* p, ull2 v) {
 }
 
 template <int W>
-using GroupSum = RowSum<W, W == 2 ? 2 : 4, W == 2 ? 4 : 2>;   // 256 words a piece of a whole wave
+using GroupSum = RowSum<W, W == 2 ? 2 : 4, 4>;   // 256 words a piece of a whole wave
 
 const int FILL_ACCESSES = 8;   // accesses per lane and component of a wave that clears: 8 KB in a row
 
@@ -644,7 +659,7 @@ void launch_few(const GradCall& c, hipStream_t s) {
 
 template <class Id>
 void launch_grouped(const GradCall& c, bool vec, char* workspace, hipStream_t s) {
-    const Grouped g = grouped_layout(workspace, c.n, c.V);
+    const Grouped g = grouped_layout(workspace, c.n, c.V, c.D);
     const Id* ids = static_cast<const Id*>(c.ids);
     const u64 words = c.V * c.D;
     if (g.one_block) {
@@ -656,12 +671,13 @@ void launch_grouped(const GradCall& c, bool vec, char* workspace, hipStream_t s)
         else launch_sum<1>(c, g, s);
         return;
     }
-    const unsigned tokens = blocks_of(c.n), clears = blocks_of(c.V + 2);
+    const unsigned tokens = blocks_of(c.n), clears = blocks_of(c.V + 3);
     const unsigned per_block = GROUP_THREADS * GROUP_TOKENS;
-    hipLaunchKernelGGL(group_clear_kernel, dim3(clears < 1024 ? clears : 1024), dim3(THREADS), 0, s, reinterpret_cast<unsigned*>(g.cursor), c.V + 2);
+    hipLaunchKernelGGL(group_clear_kernel, dim3(clears < 1024 ? clears : 1024), dim3(THREADS), 0, s, reinterpret_cast<unsigned*>(g.cursor), c.V + 3);
     hipLaunchKernelGGL(group_count_kernel<Id>, dim3((unsigned)((c.n + per_block - 1) / per_block)), dim3(GROUP_THREADS), 0, s, ids, c.n, c.V, g);
     hipLaunchKernelGGL(group_offset_kernel, dim3((unsigned)((c.V + GROUP_THREADS - 1) / GROUP_THREADS)), dim3(GROUP_THREADS), 0, s, c.V, g);
-    hipLaunchKernelGGL(group_list_kernel<Id>, dim3(tokens + (c.accumulate ? 0 : 512)), dim3(THREADS), 0, s, ids, c.n, c.V, c.D, g, tokens, c.da, c.db);
+    hipLaunchKernelGGL(group_list_kernel<Id>, dim3(tokens + 512), dim3(THREADS), 0, s, ids, c.n, c.V, c.D, g, tokens, c.accumulate,
+                       c.da, c.db);
     if (vec) launch_sum<2>(c, g, s);
     else launch_sum<1>(c, g, s);
 }
@@ -696,7 +712,7 @@ cg_status cg_share_embedding(const uint64_t* ta, const uint64_t* tb, const void*
 size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D) {
     int id = 0;
     if (check_sizes(&id, 4, n, V, D) || few(n, V, 0)) return 0;
-    return (size_t)grouped_layout(reinterpret_cast<char*>(256), n, V).bytes;
+    return (size_t)grouped_layout(reinterpret_cast<char*>(256), n, V, D).bytes;
 }
 
 cg_status cg_share_embedding_grad(const uint64_t* ga, const uint64_t* gb, const void* ids, int id_bytes, uint64_t alpha,
