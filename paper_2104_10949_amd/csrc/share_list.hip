@@ -22,13 +22,15 @@ typedef uint64_t u64;
 
 const int THREADS = 256;
 
-// Tensors of one launch, by value in the kernel's arguments (4 KB): no copy to the device, nothing to keep alive.
-const int NORM_MAX = 128, CLIP_MAX = 88;
+// Tensors of one launch, by value in the kernel's arguments (4 KB): no copy to the device, nothing to keep alive.  A tensor
+// longer than MAX_PART is several entries.
+const int NORM_MAX = 160, CLIP_MAX = 96;
+const u64 MAX_PART = (u64)1 << 31;
 
 struct NormArgs {
     const u64 *a[NORM_MAX], *b[NORM_MAX];
-    u64 n[NORM_MAX];
-    unsigned first[NORM_MAX];   // block with the tensor's first chunk
+    unsigned n[NORM_MAX];
+    unsigned first[NORM_MAX];   // block with the entry's first chunk
     unsigned keep_from;         // first block whose loads may stay in the caches
     int count;
 };
@@ -36,10 +38,11 @@ struct NormArgs {
 struct ClipArgs {
     const u64 *a[CLIP_MAX], *b[CLIP_MAX];
     u64 *za[CLIP_MAX], *zb[CLIP_MAX];
-    u64 n[CLIP_MAX];
+    unsigned n[CLIP_MAX];
     unsigned first[CLIP_MAX];
     int count;
 };
+static_assert(sizeof(NormArgs) + 16 <= 4096 && sizeof(ClipArgs) + 16 <= 4096, "kernel arguments");
 
 // tensor that a block works on
 template <class Args>
@@ -215,22 +218,26 @@ cg_status cg_share_sq_norm(const uint64_t* const* x_i, const uint64_t* const* x_
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(set_word_kernel, dim3(1), dim3(1), 0, s, z_i, (u64)0);
     const u64 chunk = chunk_words(total, 2048, 1024);
-    u64 left = total;
+    u64 left = total, done = 0;   // words of the list from here on, words of tensor k before here
     for (size_t k = 0; k < count;) {
         NormArgs t;
         t.count = 0;
         t.keep_from = ~0u;
         u64 blocks = 0;
-        for (; k < count && t.count < NORM_MAX; ++k) {
-            if (n[k] == 0) continue;
-            t.a[t.count] = x_i[k];
-            t.b[t.count] = x_ip1[k];
-            t.n[t.count] = n[k];
-            t.first[t.count++] = (unsigned)blocks;
-            if (t.keep_from == ~0u && left <= KEEP_WORDS + n[k])   // the tensor that holds the border, or the first one behind it
-                t.keep_from = (unsigned)(blocks + (left > KEEP_WORDS ? (left - KEEP_WORDS) / chunk : 0));
-            blocks += (n[k] + chunk - 1) / chunk;
-            left -= n[k];
+        while (k < count && t.count < NORM_MAX) {
+            const u64 part = n[k] - done < MAX_PART ? n[k] - done : MAX_PART;
+            if (part > 0) {
+                t.a[t.count] = x_i[k] + done;
+                t.b[t.count] = x_ip1[k] + done;
+                t.n[t.count] = (unsigned)part;
+                t.first[t.count++] = (unsigned)blocks;
+                if (t.keep_from == ~0u && left <= KEEP_WORDS + part)   // the entry that holds the border, or the first one behind it
+                    t.keep_from = (unsigned)(blocks + (left > KEEP_WORDS ? (left - KEEP_WORDS) / chunk : 0));
+                blocks += (part + chunk - 1) / chunk;
+                left -= part;
+                done += part;
+            }
+            if (done == n[k]) { ++k; done = 0; }
         }
         if (t.count > 0) hipLaunchKernelGGL(sq_norm_kernel, dim3((unsigned)blocks), dim3(THREADS), 0, s, t, chunk, z_i);
     }
@@ -260,20 +267,25 @@ cg_status cg_share_clip(const uint64_t* const* xa, const uint64_t* const* xb, co
     if (cg_status st = check_written(xa, xb, za, zb, n, count)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const u64 chunk = chunk_words(total, 16384, 1024);
+    u64 done = 0;   // words of tensor k behind here
     for (size_t next = count; next > 0;) {
         ClipArgs t;
         t.count = 0;
         u64 blocks = 0;
-        for (; next > 0 && t.count < CLIP_MAX; --next) {
+        while (next > 0 && t.count < CLIP_MAX) {
             const size_t k = next - 1;
-            if (n[k] == 0) continue;
-            t.a[t.count] = xa[k];
-            t.b[t.count] = xb[k];
-            t.za[t.count] = za[k];
-            t.zb[t.count] = zb[k];
-            t.n[t.count] = n[k];
-            t.first[t.count++] = (unsigned)blocks;
-            blocks += (n[k] + chunk - 1) / chunk;
+            const u64 part = n[k] - done < MAX_PART ? n[k] - done : MAX_PART, at = n[k] - done - part;
+            if (part > 0) {
+                t.a[t.count] = xa[k] + at;
+                t.b[t.count] = xb[k] + at;
+                t.za[t.count] = za[k] + at;
+                t.zb[t.count] = zb[k] + at;
+                t.n[t.count] = (unsigned)part;
+                t.first[t.count++] = (unsigned)blocks;
+                blocks += (part + chunk - 1) / chunk;
+                done += part;
+            }
+            if (done == n[k]) { --next; done = 0; }
         }
         if (t.count > 0) hipLaunchKernelGGL(clip_kernel, dim3((unsigned)blocks), dim3(THREADS), 0, s, t, chunk, factor);
     }

@@ -32,7 +32,7 @@ def wl():
     return workloads
 
 
-LISTS = [[], [0], [1], [2], [255, 0, 1], [4096], [4097, 3], [8191, 8193, 1, 1, 64], [100003], [1] * 300, [3000 + 7 * k for k in range(130)],
+LISTS = [[], [0], [1], [2], [255, 0, 1], [4096], [4097, 3], [8191, 8193, 1, 1, 64], [100003], [1] * 300, [3000 + 7 * k for k in range(130)], [5 + 3 * (k % 90) for k in range(161)], [64] * 97,
          [1 << 21, 5, (1 << 20) + 1], [0] * 100 + [77], list(range(200))]
 
 
@@ -71,6 +71,19 @@ def test_views_of_one_buffer_one_after_the_other(cg, ro, wl):
     cg.cg_share_clip(x, factor)
     for a, t in zip(flat, dev):
         assert np.array_equal(cg.to_host(t), a * np.uint64(7))
+
+
+def test_tensors_of_more_than_2_to_the_31_words(cg):
+    """Behind 2^34 bytes, and cut into two entries of a launch."""
+    n = (1 << 31) + 1029
+    say(f"norm and clip of a tensor of {n} words")
+    a, b = (torch.full((n,), v, dtype=torch.int64, device="cuda") for v in (3, 5))
+    for at in (0, 1 << 30, (1 << 31) - 1, 1 << 31, n - 1):
+        a[at] = 1000
+    x = cg.ShareList([a[:7], a[7:]], [b[:7], b[7:]])
+    assert int(cg.cg_share_sq_norm(x)) == (n - 5) * 3 * 13 + 5 * 1000 * 1010
+    cg.cg_share_clip(x, torch.tensor([2], device="cuda"))
+    assert int(a.sum()) == (n - 5) * 6 + 5 * 2000 and int(b.min()) == int(b.max()) == 10
 
 
 def test_lists_that_write_a_word_twice_are_refused(cg, wl):
