@@ -208,23 +208,27 @@ __device__ __forceinline__ void write_items(Item* items, unsigned row, unsigned 
     for (unsigned k = 0; k < m; ++k) items[k] = {row, first + k * most, k + 1 < m ? most : c - k * most, m == 1};
 }
 
+// The part of the n accesses at p that falls to this block, of all but the first.
+template <class T>
+__device__ __forceinline__ void clear_stretch(T* p, u64 n) {
+    const u64 each = (n + gridDim.x - 2) / (gridDim.x - 1), begin = (blockIdx.x - 1) * each, end = begin + each < n ? begin + each : n;
+    for (u64 i = begin + threadIdx.x; i < end; i += GROUP_THREADS) __builtin_nontemporal_store(T(0), p + i);
+}
+
 // Few tokens: the first block groups them all, while the others clear the gradient (no block is one that clears if it
 // is added to).  The rows with tokens are cleared, too: they are few where the table is large.
 template <class Id>
 __global__ __launch_bounds__(GROUP_THREADS) void group_few_kernel(const Id* __restrict__ ids, u64 n, u64 V, Grouped g,
                                                                   u64* da, u64* db, u64 words, bool pairs) {
     if (blockIdx.x > 0) {
-        const u64 step = (u64)(gridDim.x - 1) * GROUP_THREADS, i0 = (u64)(blockIdx.x - 1) * GROUP_THREADS + threadIdx.x;
-        if (pairs)
-            for (u64 i = i0; i < words / 2; i += step) {
-                __builtin_nontemporal_store(ull2(0), reinterpret_cast<ull2*>(da) + i);
-                __builtin_nontemporal_store(ull2(0), reinterpret_cast<ull2*>(db) + i);
-            }
-        else
-            for (u64 i = i0; i < words; i += step) {
-                __builtin_nontemporal_store((u64)0, da + i);
-                __builtin_nontemporal_store((u64)0, db + i);
-            }
+        // a stretch of either component per block (75 -> 70 us for 393 MB against blocks that take turns)
+        if (pairs) {
+            clear_stretch(reinterpret_cast<ull2*>(da), words / 2);
+            clear_stretch(reinterpret_cast<ull2*>(db), words / 2);
+        } else {
+            clear_stretch(da, words);
+            clear_stretch(db, words);
+        }
         return;
     }
     __shared__ unsigned key[TABLE], count[TABLE];
