@@ -59,7 +59,7 @@ __global__ __launch_bounds__(THREADS) void sq_sum_kernel(HeadParams p, int lg) {
             for (int u = 0; u < SQ_UNROLL; ++u) {
                 const unsigned c = i + (u << lg);
                 x[u] = y[u] = T(0);
-                if (c < units) { x[u] = __builtin_nontemporal_load(a + c); y[u] = __builtin_nontemporal_load(b + c); }
+                if (c < units) { x[u] = a[c]; y[u] = b[c]; }
             }
 #pragma unroll
             for (int u = 0; u < SQ_UNROLL; ++u) sum += x[u] * (x[u] + 2 * y[u]);

@@ -161,34 +161,52 @@ __global__ void clip_factor_kernel(const u64* s0, const u64* s1, const u64* s2, 
 // ---- host ----
 struct Range {
     uintptr_t begin, end;
-    size_t entry;    // which tensor
-    int part;        // 0, 1: the components read; 2, 3: the components written
+    bool written;
     bool operator<(const Range& o) const { return begin < o.begin; }
 };
 
+// Do lists that lie one behind the other, as views of one buffer per component do, meet?  True if none of them can: every
+// list of outputs ascends without overlap, and its hull meets no other list's (an input that is its own output aside).
+bool lists_apart(const u64* const* const* lists, const size_t* n, size_t count) {
+    uintptr_t lo[4], hi[4];
+    for (int p = 0; p < 4; ++p) {
+        lo[p] = UINTPTR_MAX;
+        hi[p] = 0;
+        for (size_t k = 0; k < count; ++k) {
+            if (n[k] == 0 || (p < 2 && lists[p][k] == lists[p + 2][k])) continue;
+            const uintptr_t b = reinterpret_cast<uintptr_t>(lists[p][k]), e = b + n[k] * 8;
+            if (p >= 2 && b < hi[p]) return false;
+            if (b < lo[p]) lo[p] = b;
+            if (e > hi[p]) hi[p] = e;
+        }
+    }
+    for (int p = 2; p < 4; ++p)
+        for (int q = 0; q < p; ++q)
+            if (lo[p] < hi[q] && lo[q] < hi[p]) return false;
+    return true;
+}
+
 // Every word that is written is written once and read by nobody else: outputs meet neither each other nor an input,
 // except an output equal to the input of its own position.
-cg_status check_written(const u64* const* xa, const u64* const* xb, u64* const* za, u64* const* zb, const size_t* n,
-                        size_t count) {
+cg_status check_written(const u64* const* const* lists, const size_t* n, size_t count) {
+    if (lists_apart(lists, n, count)) return CG_OK;
     Range* r = static_cast<Range*>(malloc(4 * count * sizeof(Range)));
     if (!r) return CG_ERR_DEVICE;
     size_t m = 0;
     for (size_t k = 0; k < count; ++k) {
         if (n[k] == 0) continue;
-        const void* p[4] = {xa[k], xb[k], za[k], zb[k]};
         for (int part = 0; part < 4; ++part) {
-            if (part < 2 && p[part] == p[part + 2]) continue;   // in place
-            const uintptr_t b = reinterpret_cast<uintptr_t>(p[part]);
-            r[m++] = {b, b + n[k] * 8, k, part};
+            if (part < 2 && lists[part][k] == lists[part + 2][k]) continue;   // in place
+            const uintptr_t b = reinterpret_cast<uintptr_t>(lists[part][k]);
+            r[m++] = {b, b + n[k] * 8, part >= 2};
         }
     }
     std::sort(r, r + m);
     uintptr_t read_end = 0, written_end = 0;
     bool bad = false;
     for (size_t i = 0; i < m && !bad; ++i) {
-        const bool written = r[i].part >= 2;
-        bad = r[i].begin < written_end || (written && r[i].begin < read_end);
-        uintptr_t& end = written ? written_end : read_end;
+        bad = r[i].begin < written_end || (r[i].written && r[i].begin < read_end);
+        uintptr_t& end = r[i].written ? written_end : read_end;
         if (r[i].end > end) end = r[i].end;
     }
     free(r);
@@ -280,7 +298,7 @@ cg_status cg_share_clip(const uint64_t* const* xa, const uint64_t* const* xb, co
     for (size_t k = 0; k < count; ++k)
         if (n[k] > 0 && (cg::overlap(factor, 8, za[k], n[k] * 8) || cg::overlap(factor, 8, zb[k], n[k] * 8))) return CG_ERR_ALIAS;
     if (total == 0) return CG_OK;
-    if (cg_status st = check_written(xa, xb, za, zb, n, count)) return st;
+    if (cg_status st = check_written(lists, n, count)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const u64 chunk = chunk_words(total, 16384, 1024);
     u64 done = 0;   // words of tensor k behind here

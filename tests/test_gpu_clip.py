@@ -86,6 +86,21 @@ def test_tensors_of_more_than_2_to_the_31_words(cg):
     assert int(a.sum()) == (n - 5) * 6 + 5 * 2000 and int(b.min()) == int(b.max()) == 10
 
 
+def test_lists_in_any_order(cg, wl):
+    """Outputs that descend, lie between the inputs or are the inputs of their own position are all fine."""
+    host = [wl.draw_ring((100,), 330 + k) for k in range(4)]
+    buffer = torch.zeros(1000, dtype=torch.int64, device="cuda")
+    a0, a1, b0, b1 = (buffer[200 * k:200 * k + 100] for k in range(4))
+    for t, h in zip((a0, a1, b0, b1), host):
+        t.copy_(cg.to_device(h))
+    y0, y1 = buffer[900:1000], buffer[100:200]
+    factor = torch.tensor([3], device="cuda")
+    cg.cg_share_clip(cg.ShareList([a0, a1], [b0, b1]), factor, cg.ShareList([y0, y1], [b0, b1]))
+    for t, h in zip((y0, y1, b0, b1), host):
+        assert np.array_equal(cg.to_host(t), h * np.uint64(3))
+    assert np.array_equal(cg.to_host(a0), host[0]) and not bool(buffer[300:400].any())
+
+
 def test_lists_that_write_a_word_twice_are_refused(cg, wl):
     t = [torch.ones(64, dtype=torch.int64, device="cuda") for _ in range(2)]
     factor = torch.tensor([2], device="cuda")

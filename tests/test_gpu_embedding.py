@@ -223,6 +223,32 @@ def test_gradient_in_two_graphs(cg, ro, wl, n):
                 assert np.array_equal(cg.to_host(t), want), first_mismatch(cg.to_host(t), want)
 
 
+@pytest.mark.parametrize("n", [500, 3000, 9000])
+def test_calls_captured_as_they_are(cg, ro, wl, n):
+    """Lookup and gradient captured without a word about scratch memory: nothing is allocated inside the call for it."""
+    say(f"lookup and gradient of {n} tokens in a graph")
+    V, D = 70, 18
+    T = [wl.draw_ring((V, D), 190 + c) for c in range(2)]
+    G = [wl.draw_ring((n, D), 192 + c) for c in range(2)]
+    table, g = [cg.to_device(t) for t in T], [cg.to_device(t) for t in G]
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    cg.cg_share_embedding_grad(*g, ids, V, 3)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        z = cg.cg_share_embedding(*table, ids, 9)
+        d = cg.cg_share_embedding_grad(*g, ids, V, 3)
+    for turn, kind in enumerate(("rank", "mixed", "one", "position")):
+        host = draw_ids(kind, n, V, turn).clip(-5, V + 5)
+        ids.copy_(torch.from_numpy(host))
+        graph.replay()
+        _ = cg.cg_share_embedding_grad(*g, ids, V, 3)
+        for a, t in zip(z, T):
+            assert np.array_equal(cg.to_host(a), ro.embedding(t, host, 9))
+        for a, h in zip(d, G):
+            assert np.array_equal(cg.to_host(a), ro.embedding_grad(h, host, V, 3))
+
+
 def test_gradient_of_many_words(cg):
     """Gradients behind 2^32 bytes and a table of as many: rows of ones, so that every sum is a count."""
     n, V, D = 1 << 16, (1 << 17) + 1, 8200

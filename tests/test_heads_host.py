@@ -136,6 +136,11 @@ def test_norm_and_clip_validation(b):
     for bad in ([5 * P, 5 * P + 72], [5 * P, 5 * P], [5 * P, 7 * P], [5 * P, P + 8], [P + 8, 6 * P], [3 * P, 6 * P], [2 * P, 6 * P]):
         assert clip(xa, xb, 9 * P, arrays(bad)[0], zb, n, 2, None) == b.CG_ERR_ALIAS, bad
     assert clip(*arrays([P, P], [3 * P, 4 * P]), 9 * P, *arrays([P, P], [7 * P, 8 * P]), sizes(10, 10), 2, None) == b.CG_ERR_ALIAS  # twice in place
+    # in place over the other entry's input, an output before the one in front of it, inputs between outputs
+    assert clip(*arrays([P, 2 * P], [3 * P, 4 * P]), 9 * P, *arrays([2 * P, P], [7 * P, 8 * P]), n, 2, None) == b.CG_ERR_ALIAS
+    assert clip(*arrays([P, 2 * P], [3 * P, 4 * P]), 9 * P, *arrays([6 * P, 6 * P - 152], [7 * P, 8 * P]), n, 2, None) == b.CG_ERR_ALIAS
+    assert clip(*arrays([P, 2 * P], [3 * P, 4 * P]), 9 * P, *arrays([P, 2 * P], [3 * P + 8, 8 * P]), n, 2, None) == b.CG_ERR_ALIAS
+    assert clip(*arrays([P, 2 * P], [3 * P, 4 * P]), 9 * P, *arrays([P, 2 * P], [P + 80 - 8, 8 * P]), n, 2, None) == b.CG_ERR_ALIAS
     assert clip(None, None, 9 * P, None, None, None, 0, None) == b.CG_OK
     assert clip(xa, xb, 9 * P, za, zb, sizes(0, 0), 2, None) == b.CG_OK
     assert factor(P, 2 * P, 3 * P, 1, 16, 0, None) == b.CG_ERR_NULL
