@@ -42,7 +42,7 @@ struct ClipArgs {
     unsigned first[CLIP_MAX];
     int count;
 };
-static_assert(sizeof(NormArgs) + 16 <= 4096 && sizeof(ClipArgs) + 16 <= 4096, "kernel arguments");
+static_assert(sizeof(NormArgs) + 32 <= 4096 && sizeof(ClipArgs) + 16 <= 4096, "kernel arguments");
 
 // tensor that a block works on
 template <class Args>
@@ -95,18 +95,23 @@ __device__ __forceinline__ u64 sum_of_squares(const u64* __restrict__ a, const u
     return sum;
 }
 
-__global__ __launch_bounds__(NORM_THREADS) void sq_norm_kernel(NormArgs t, u64 chunk, u64* z) {
-    const int k = tensor_of(t, blockIdx.x);
-    const u64 begin = (u64)(blockIdx.x - t.first[k]) * chunk, end = begin + chunk < t.n[k] ? begin + chunk : t.n[k];
-    u64 sum = blockIdx.x >= t.keep_from ? sum_of_squares<true>(t.a[k], t.b[k], begin + threadIdx.x, end)
-                                        : sum_of_squares<false>(t.a[k], t.b[k], begin + threadIdx.x, end);
+// Chunk by chunk; `alone`: one block has all of them and its sum is the result.
+__global__ __launch_bounds__(NORM_THREADS) void sq_norm_kernel(NormArgs t, unsigned chunks, u64 chunk, bool alone, u64* z) {
+    u64 sum = 0;
+    for (unsigned b = blockIdx.x; b < chunks; b += gridDim.x) {
+        const int k = tensor_of(t, b);
+        const u64 begin = (u64)(b - t.first[k]) * chunk, end = begin + chunk < t.n[k] ? begin + chunk : t.n[k];
+        sum += b >= t.keep_from ? sum_of_squares<true>(t.a[k], t.b[k], begin + threadIdx.x, end)
+                                : sum_of_squares<false>(t.a[k], t.b[k], begin + threadIdx.x, end);
+    }
     for (int h = 32; h > 0; h >>= 1) sum += __shfl_xor((unsigned long long)sum, h);
     __shared__ u64 part[NORM_THREADS / 64];
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int w = 1; w < NORM_THREADS / 64; ++w) sum += part[w];
-        atomicAdd(reinterpret_cast<unsigned long long*>(z), (unsigned long long)sum);
+        if (alone) *z = sum;
+        else atomicAdd(reinterpret_cast<unsigned long long*>(z), (unsigned long long)sum);
     }
 }
 
@@ -250,8 +255,12 @@ cg_status cg_share_sq_norm(const uint64_t* const* x_i, const uint64_t* const* x_
     for (size_t k = 0; k < count; ++k)
         if (n[k] > 0 && (cg::overlap(z_i, 8, x_i[k], n[k] * 8) || cg::overlap(z_i, 8, x_ip1[k], n[k] * 8))) return CG_ERR_ALIAS;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(set_word_kernel, dim3(1), dim3(1), 0, s, z_i, (u64)0);
     const u64 chunk = chunk_words(total, 1024, NORM_UNROLL * NORM_THREADS);
+    // up to four chunks, a round trip to memory each, are less than a launch that clears the word
+    u64 chunks = 0;
+    for (size_t k = 0; k < count && chunks <= 4; ++k) chunks += (n[k] + chunk - 1) / chunk;
+    const bool alone = chunks >= 1 && chunks <= 4;   // of at most four tensors, hence one launch
+    if (!alone) hipLaunchKernelGGL(set_word_kernel, dim3(1), dim3(1), 0, s, z_i, (u64)0);
     u64 left = total, done = 0;   // words of the list from here on, words of tensor k before here
     for (size_t k = 0; k < count;) {
         NormArgs t;
@@ -273,7 +282,8 @@ cg_status cg_share_sq_norm(const uint64_t* const* x_i, const uint64_t* const* x_
             }
             if (done == n[k]) { ++k; done = 0; }
         }
-        if (t.count > 0) hipLaunchKernelGGL(sq_norm_kernel, dim3((unsigned)blocks), dim3(NORM_THREADS), 0, s, t, chunk, z_i);
+        if (t.count > 0)
+            hipLaunchKernelGGL(sq_norm_kernel, dim3(alone ? 1 : (unsigned)blocks), dim3(NORM_THREADS), 0, s, t, (unsigned)blocks, chunk, alone, z_i);
     }
     return hipGetLastError() == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }

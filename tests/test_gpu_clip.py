@@ -32,7 +32,7 @@ def wl():
     return workloads
 
 
-LISTS = [[], [0], [1], [2], [255, 0, 1], [4096], [4097, 3], [8191, 8193, 1, 1, 64], [100003], [1] * 300, [3000 + 7 * k for k in range(130)], [5 + 3 * (k % 90) for k in range(161)], [64] * 97,
+LISTS = [[], [0], [1], [2], [255, 0, 1], [4096], [4097, 3], [8191, 8193, 1, 1, 64], [100003], [1] * 300, [3000 + 7 * k for k in range(130)], [5 + 3 * (k % 90) for k in range(161)], [64] * 97, [3 * 8192, 1], [4 * 8192 + 1], [9000, 0, 16384],
          [1 << 21, 5, (1 << 20) + 1], [0] * 100 + [77], list(range(200))]
 
 
