@@ -60,10 +60,11 @@ __global__ void set_word_kernel(u64* z, u64 v) { *z = v; }
 const int NORM_UNROLL = 8;   // loads of each component under way per lane
 
 // Clipping reads what the norm has read, as soon as the factor is there.  The norm's last KEEP_WORDS elements (both
-// components, 192 MB of the 256 MB that the memory-side cache holds) are therefore read as what is wanted again, and
-// clipping begins at the end; what lies before them streams past the caches.  19.3 million elements: norm + clipping
-// 89 + 102 us with plain accesses from the beginning, 55 + 117 us with all of the norm streaming, 55 + 95 us this way.
-const u64 KEEP_WORDS = (u64)12 << 20;
+// components, 64 MB of the 256 MB that the memory-side cache holds) are therefore read as what is wanted again, and
+// clipping begins at the end; what lies before them streams past the caches, which is faster for the norm.  Norm of 25.5
+// million elements alone, norm and clipping of 19.3 million: 68, 53 and 102 us with all of it streaming, 68, 54 and 101 this way,
+// 74, 55 and 97 with 192 MB kept; with plain accesses and clipping from the beginning 82, 87 and 101.
+const u64 KEEP_WORDS = (u64)4 << 20;
 
 template <bool KEEP>
 __device__ __forceinline__ u64 load(const u64* p) {
