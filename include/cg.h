@@ -596,11 +596,11 @@ CG_API cg_status cg_breshare(const uint64_t *z_i, const uint8_t *key_self, const
  * nothing, the gradient without accumulate is zero.
  *
  * The gradient groups the tokens by id in scratch memory (device memory, 16-byte aligned, not
- * overlapping an operand: CG_ERR_ALIAS) of cg_share_embedding_grad_workspace_bytes(n, V, D) bytes, whose
- * contents are undefined afterwards; calls that may overlap in time, captured ones among
- * them, need one each.  With less, misaligned, or none (NULL) it adds every token's row to the table word by word:
- * the same bits, slower.  The query returns 0 for sizes where scratch memory is of no use, and for
- * invalid ones.
+ * overlapping an operand: CG_ERR_ALIAS) of cg_share_embedding_grad_workspace_bytes(n, V, D, accumulate)
+ * bytes, whose contents are undefined afterwards; calls that may overlap in time, captured ones among
+ * them, need one each.  With less, misaligned, or none (NULL) it adds every token's row to the table word by
+ * word: the same bits, slower.  The query returns 0 for sizes where scratch memory is of no use (few tokens),
+ * and for invalid ones.
  */
 CG_API cg_status cg_share_embedding(const uint64_t *ta, const uint64_t *tb, const void *ids, int id_bytes,
                              uint64_t alpha, uint64_t *za, uint64_t *zb, size_t n, size_t V, size_t D,
@@ -610,7 +610,7 @@ CG_API cg_status cg_share_embedding_grad(const uint64_t *ga, const uint64_t *gb,
                                   uint64_t alpha, uint64_t *da, uint64_t *db, size_t n, size_t V, size_t D,
                                   int accumulate, void *workspace, size_t workspace_bytes, void *stream);
 
-CG_API size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D);
+CG_API size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D, int accumulate);
 
 /*
  * Norms of query and key heads with the position rotation, around the protocol that finds the

@@ -119,7 +119,7 @@ def lib() -> ctypes.CDLL:
         L.cg_share_conv2d_wgrad.argtypes = [vp] * 5 + [ctypes.POINTER(ConvDesc), vp]
         L.cg_share_embedding.argtypes = [vp] * 3 + [ctypes.c_int, u64, vp, vp, sz, sz, sz, vp]
         L.cg_share_embedding_grad.argtypes = [vp] * 3 + [ctypes.c_int, u64, vp, vp, sz, sz, sz, ctypes.c_int, vp, sz, vp]
-        L.cg_share_embedding_grad_workspace_bytes.argtypes = [sz] * 3
+        L.cg_share_embedding_grad_workspace_bytes.argtypes = [sz] * 3 + [ctypes.c_int]
         head = ctypes.POINTER(HeadDesc)
         L.cg_share_head_sq_sum.argtypes = [vp] * 3 + [i64] * 4 + [vp]
         L.cg_share_head_norm_rotate.argtypes = [vp] * 8 + [head, vp]
@@ -707,15 +707,15 @@ def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=Non
     ip, width = _index_ptr(ids)
     n = ids.numel()
     if workspace is None:
-        workspace = _scratch(lib().cg_share_embedding_grad_workspace_bytes(n, V, D), ga.device, stream)
+        workspace = _scratch(lib().cg_share_embedding_grad_workspace_bytes(n, V, D, accumulate), ga.device, stream)
     wp, wb = _ws(workspace)
     _check(lib().cg_share_embedding_grad(pga, pgb, ip, width, int(alpha) % (1 << 64), pda, pdb, n, V, D,
                                          int(bool(accumulate)), wp, wb, _stream(stream)), "cg_share_embedding_grad")
     return da, db
 
 
-def cg_share_embedding_grad_workspace_bytes(n: int, V: int, D: int) -> int:
-    return int(lib().cg_share_embedding_grad_workspace_bytes(n, V, D))
+def cg_share_embedding_grad_workspace_bytes(n: int, V: int, D: int, accumulate: bool = False) -> int:
+    return int(lib().cg_share_embedding_grad_workspace_bytes(n, V, D, bool(accumulate)))
 
 
 def _row_step(t: torch.Tensor) -> int:

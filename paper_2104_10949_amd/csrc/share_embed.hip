@@ -77,8 +77,9 @@ __global__ __launch_bounds__(THREADS) void clear_kernel(u64* a, u64* b, u64 n) {
     }
 }
 
-// Gradient without scratch memory, many tokens: every token's row is added to its row of the table's gradient, word by word, a
-// wave's atomics on 64 words in a row.  65536 tokens of 32000 x 1024: 833 us, 308 with scratch memory (two words a lane: 1670).
+// Gradient word by word: every token's row is added to its row of the table's gradient, a wave's atomics on 64 words in a row.
+// For few words that are added to a table, and where there is no scratch memory: 65536 tokens of 32000 x 1024: 833 us, 308
+// with scratch memory (two words a lane: 1670).
 template <class Id>
 __global__ __launch_bounds__(THREADS) void embed_grad_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
                                                              const Id* __restrict__ ids, u64 alpha, u64* da, u64* db,
@@ -481,12 +482,12 @@ void launch_embed(const u64* ta, const u64* tb, const void* ids, u64 alpha, u64*
                        dim3(THREADS), 0, s, ta, tb, static_cast<const Id*>(ids), alpha, za, zb, n, V, D, lg);
 }
 
-// ---- gradient of few tokens: one launch, no scratch memory ----
+// ---- gradient of few tokens, written in full: one launch, no scratch memory ----
 // The first blocks hold all ids in LDS, and each of their waves has a token and a share of its row: ballots over the ids name
 // the tokens of the same row, and the first of them adds them all up.  A row with more than OWN tokens waits until the
-// block has come to its end: then the waves share its tokens out and meet in LDS (777 tokens of 1531 x 515, 73 of them the same:
-// 19 us in two launches by way of a list, 14 us this way).  The other blocks clear the rows without tokens, which they know
-// from one bit per row in LDS.
+// block has come to its end: then the waves share its tokens out and meet in LDS.  The other blocks clear the rows without
+// tokens, which they know from one bit per row in LDS.  (777 tokens of 1531 x 515: 14 us, 19 in two launches by way of a
+// list; clearing and then adding word by word is 16 us there, 15 instead of 12 at 16 to 256 tokens.)
 const int FEW = 1024, FEW_THREADS = 512, WAVES = FEW_THREADS / 64;
 const int FEW_ROWS = 1 << 18;
 // Sixteen rows under way at a time and pieces of one access per lane: what counts in these calls is the time of a round trip to
@@ -499,8 +500,8 @@ const int OWN = 8;
 template <class Id, int W>
 __global__ __launch_bounds__(FEW_THREADS) void few_sum_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
                                                               const Id* __restrict__ ids, u64 alpha, u64* da, u64* db, unsigned n,
-                                                              u64 V, u64 D, int accumulate, unsigned pieces, unsigned pieces_each,
-                                                              unsigned shares, unsigned sum_blocks) {
+                                                              u64 V, u64 D, unsigned pieces, unsigned pieces_each, unsigned shares,
+                                                              unsigned sum_blocks) {
     typedef typename Words<W>::type T;
     typedef FewSum<W> Sum;
     const int U = Sum::U, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -534,9 +535,8 @@ __global__ __launch_bounds__(FEW_THREADS) void few_sum_kernel(const u64* __restr
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (c0 + u * 64 >= units) continue;
-            const T x = sum.a[u] * alpha, y = sum.b[u] * alpha;
-            if (accumulate) { pa[c[u]] += x; pb[c[u]] += y; }
-            else { __builtin_nontemporal_store(x, pa + c[u]); __builtin_nontemporal_store(y, pb + c[u]); }
+            __builtin_nontemporal_store(sum.a[u] * alpha, pa + c[u]);
+            __builtin_nontemporal_store(sum.b[u] * alpha, pb + c[u]);
         }
     };
     const auto columns = [&](unsigned c0, u64 (&c)[U]) {
@@ -627,6 +627,9 @@ struct GradCall {
     int accumulate;
 };
 
+// Blocks of a kernel whose threads take words in turn.
+unsigned few_blocks(u64 words) { return (unsigned)((words < 4096 * THREADS ? words + THREADS - 1 : 4096 * THREADS) / THREADS); }
+
 unsigned blocks_of(u64 threads) { return (unsigned)((threads + THREADS - 1) / THREADS); }
 
 template <int W>
@@ -647,8 +650,18 @@ void launch_sum(const GradCall& c, const Grouped& g, hipStream_t s) {
                            (unsigned)pieces, (unsigned)items, g);
 }
 
-// One launch without scratch memory: where the ids, and a bit per row that may have to be cleared, fit the LDS.
-bool few(u64 n, u64 V, int accumulate) { return n <= (u64)FEW && (accumulate || V <= (u64)FEW_ROWS); }
+// The way of a call, by its sizes.
+enum Route { FEW_TOKENS, WORD_BY_WORD, GROUPED };
+
+// Words of gradient up to which adding to a table word by word, in one launch, is as fast as grouping (2000 tokens of 64 words 12 us
+// against 19, of 515 words 20 and 22; 4000 of 768 words 45 and 34), and tokens up to which it does not suffer too much where
+// all of them are the same (2000 of 64 words 53 us and 36, 4000: 104 and 61).
+const u64 FEW_WORDS = 1 << 20, FEW_ADDED = 2048;
+
+Route route_of(u64 n, u64 V, u64 D, bool accumulate) {
+    if (!accumulate) return n <= (u64)FEW && V <= (u64)FEW_ROWS ? FEW_TOKENS : GROUPED;
+    return n <= FEW_ADDED && n * D <= FEW_WORDS ? WORD_BY_WORD : GROUPED;
+}
 
 template <class Id, int W>
 void launch_few(const GradCall& c, hipStream_t s) {
@@ -657,10 +670,10 @@ void launch_few(const GradCall& c, hipStream_t s) {
     u64 each = c.n * pieces / 8192;
     each = each < 1 ? 1 : each < pieces ? each : pieces;
     const u64 shares = (pieces + each - 1) / each, sums = (c.n * shares + WAVES - 1) / WAVES, per_fill = (u64)FILL_ACCESSES * FEW_THREADS;
-    u64 fills = c.accumulate ? 0 : (c.V * units + per_fill - 1) / per_fill;
+    u64 fills = (c.V * units + per_fill - 1) / per_fill;
     if (fills > 2048) fills = 2048;
     hipLaunchKernelGGL((few_sum_kernel<Id, W>), dim3((unsigned)(sums + fills)), dim3(FEW_THREADS), 0, s, c.ga, c.gb, static_cast<const Id*>(c.ids),
-                       c.alpha, c.da, c.db, (unsigned)c.n, c.V, c.D, c.accumulate, (unsigned)pieces, (unsigned)each, (unsigned)shares, (unsigned)sums);
+                       c.alpha, c.da, c.db, (unsigned)c.n, c.V, c.D, (unsigned)pieces, (unsigned)each, (unsigned)shares, (unsigned)sums);
 }
 
 template <class Id>
@@ -715,9 +728,9 @@ cg_status cg_share_embedding(const uint64_t* ta, const uint64_t* tb, const void*
     return launched();
 }
 
-size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D) {
+size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t D, int accumulate) {
     int id = 0;
-    if (check_sizes(&id, 4, n, V, D) || few(n, V, 0)) return 0;
+    if (n == 0 || check_sizes(&id, 4, n, V, D) || route_of(n, V, D, accumulate != 0) != GROUPED) return 0;
     return (size_t)grouped_layout(reinterpret_cast<char*>(256), n, V, D).bytes;
 }
 
@@ -739,7 +752,7 @@ cg_status cg_share_embedding_grad(const uint64_t* ga, const uint64_t* gb, const 
                 return CG_ERR_ALIAS;
         vec = vec && all_aligned16(in, 2);
     }
-    const u64 need = cg_share_embedding_grad_workspace_bytes(n, V, D);
+    const u64 need = cg_share_embedding_grad_workspace_bytes(n, V, D, accumulate);
     const bool scratch = need > 0 && workspace && workspace_bytes >= need && aligned(workspace, 16);
     if (scratch) {
         const void* operands[5] = {ga, gb, ids, da, db};
@@ -749,7 +762,7 @@ cg_status cg_share_embedding_grad(const uint64_t* ga, const uint64_t* gb, const 
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
     const GradCall c = {ga, gb, ids, alpha, da, db, n, V, D, accumulate};
-    if (n > 0 && few(n, V, accumulate)) {
+    if (n > 0 && route_of(n, V, D, accumulate) == FEW_TOKENS) {
         if (id_bytes == 8) {
             if (vec) launch_few<long long, 2>(c, s);
             else launch_few<long long, 1>(c, s);
@@ -764,14 +777,14 @@ cg_status cg_share_embedding_grad(const uint64_t* ga, const uint64_t* gb, const 
         else launch_grouped<int>(c, vec, static_cast<char*>(workspace), s);
         return launched();
     }
-    if (!accumulate) hipLaunchKernelGGL(clear_kernel, dim3(2048), dim3(THREADS), 0, s, da, db, (u64)V * D);
+    if (!accumulate) hipLaunchKernelGGL(clear_kernel, dim3(few_blocks((u64)V * D)), dim3(THREADS), 0, s, da, db, (u64)V * D);
     if (n > 0) {
+        const dim3 grid(few_blocks((u64)n * D));
         if (id_bytes == 8)
-            hipLaunchKernelGGL(embed_grad_kernel<long long>, dim3(4096), dim3(THREADS), 0, s, ga, gb,
-                               static_cast<const long long*>(ids), alpha, da, db, n, V, D);
+            hipLaunchKernelGGL(embed_grad_kernel<long long>, grid, dim3(THREADS), 0, s, ga, gb, static_cast<const long long*>(ids), alpha, da,
+                               db, n, V, D);
         else
-            hipLaunchKernelGGL(embed_grad_kernel<int>, dim3(4096), dim3(THREADS), 0, s, ga, gb,
-                               static_cast<const int*>(ids), alpha, da, db, n, V, D);
+            hipLaunchKernelGGL(embed_grad_kernel<int>, grid, dim3(THREADS), 0, s, ga, gb, static_cast<const int*>(ids), alpha, da, db, n, V, D);
     }
     return launched();
 }

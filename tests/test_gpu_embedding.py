@@ -118,7 +118,7 @@ def test_lookup_beyond_32_bit_offsets(cg):
 
 
 # (n, V, D): one token to many, rows shorter and longer than a wave's piece, tables smaller and larger than the batch
-GRADS = [(1, 1, 1), (1, 700, 512), (2, 5, 3), (63, 7, 16), (64, 64, 64), (65, 1000, 30), (128, 300, 514), (129, 300, 514), (100, 40, 1031), (500, 3, 515), (777, 1531, 130), (1024, 2000, 257), (1025, 100, 260), (1024, 3, 70000), (600, (1 << 18) + 5, 4), (600, 1 << 18, 4), (2048, 100, 258),
+GRADS = [(1, 1, 1), (1, 700, 512), (2, 5, 3), (63, 7, 16), (64, 64, 64), (65, 1000, 30), (128, 300, 514), (129, 300, 514), (100, 40, 1031), (500, 3, 515), (777, 1531, 130), (1024, 2000, 257), (1025, 100, 260), (1024, 3, 70000), (600, (1 << 18) + 5, 4), (600, 1 << 18, 4), (2048, 60, 512), (2048, 60, 513), (2049, 60, 8), (2048, 100, 258),
          (4096, 300, 8), (4097, 40, 64), (5000, 5000, 20), (3000, 9, 1030), (9001, 2000, 33), (20000, 700, 34), (16384, 16384, 6), (40000, 50, 18)]
 
 
@@ -132,7 +132,7 @@ def test_gradient(cg, ro, wl, n, V, D, kind, scratch):
     dev = torch.from_numpy(ids).to("cuda").to(torch.int32 if kind == "rank" else torch.int64)
     g = [place(cg, t, words) for t in G]
     d = [Guarded((V, D), words) for _ in range(2)]
-    need = cg.cg_share_embedding_grad_workspace_bytes(n, V, D) if scratch else 0
+    need = max(cg.cg_share_embedding_grad_workspace_bytes(n, V, D, acc) for acc in (False, True)) if scratch else 0
     memory = torch.full((need + 512,), 0x5A, dtype=torch.uint8, device="cuda")
     ws = memory[256:256 + need]                              # without: none of it is used
     cg.cg_share_embedding_grad(*g, dev, V, alpha, da=d[0].t, db=d[1].t, workspace=ws)
@@ -193,7 +193,7 @@ def test_gradient_in_two_graphs(cg, ro, wl, n):
     for k in range(2):
         ids = torch.from_numpy(draw_ids("rank", n, V, k)).cuda()
         # the second graph has scratch memory of its own, the first none
-        ws = torch.empty(cg.cg_share_embedding_grad_workspace_bytes(n, V, D) if k else 0, dtype=torch.uint8, device="cuda")
+        ws = torch.empty(cg.cg_share_embedding_grad_workspace_bytes(n, V, D, True) if k else 0, dtype=torch.uint8, device="cuda")
         g = [cg.to_device(wl.draw_ring((n, D), 160 + c)) for c in range(2)]
         d = [torch.zeros((V, D), dtype=torch.int64, device="cuda") for _ in range(2)]
         cg.cg_share_embedding_grad(*g, ids, V, 3, da=d[0], db=d[1], workspace=ws)

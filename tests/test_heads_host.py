@@ -63,7 +63,8 @@ def test_embedding_gradient_validation(b):
     for where in (P, 2 * P + n * D * 8 - 16, 3 * P + 16, 4 * P, 5 * P - need(n, V, D) + 16):
         assert call(n=n, V=V, D=D, ws=where, bytes=need(n, V, D)) == b.CG_ERR_ALIAS
     assert need(0, 5, 5) == need(5000, 0, 5) == need(5000, 5, 0) == need(1 << 31, 5, 5) == need(5000, 5, (1 << 22) + 1) == 0
-    assert need(1024, 5, 5) == 0 < need(1025, 5, 5)
+    assert need(1024, 1 << 18, 5) == 0 < min(need(1025, 5, 5), need(1024, (1 << 18) + 1, 5))
+    assert need(2048, 5, 512, True) == need(1, 1 << 30, 9, True) == 0 < min(need(2049, 5, 5, True), need(2048, 5, 513, True))
 
 
 def desc(b, **kw):
