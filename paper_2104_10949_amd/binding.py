@@ -294,7 +294,7 @@ def _ws(workspace) -> Tuple[int, int]:
 
 SCRATCH_LIMIT = 4 << 30   # bytes: a call that would take more runs without
 SCRATCH_SPARE = 8         # ... and so does one that would leave less than this part of the card's memory free
-SCRATCH_SMALL = 1 << 20   # bytes: a call that takes no more does not ask how much is free (its outputs come from the same cache)
+SCRATCH_SMALL = 1 << 20   # bytes: up to here it is a block of the allocator's pool for small tensors, and no one asks how much is free
 
 
 def _scratch_fits(nbytes: int, device) -> bool:
@@ -708,6 +708,8 @@ def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=Non
     n = ids.numel()
     if workspace is None:
         workspace = _scratch(lib().cg_share_embedding_grad_workspace_bytes(n, V, D, accumulate), ga.device, stream)
+    else:
+        _current(workspace)
     wp, wb = _ws(workspace)
     _check(lib().cg_share_embedding_grad(pga, pgb, ip, width, int(alpha) % (1 << 64), pda, pdb, n, V, D,
                                          int(bool(accumulate)), wp, wb, _stream(stream)), "cg_share_embedding_grad")

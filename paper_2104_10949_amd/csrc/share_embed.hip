@@ -77,6 +77,14 @@ __global__ __launch_bounds__(THREADS) void clear_kernel(u64* a, u64* b, u64 n) {
     }
 }
 
+__device__ __forceinline__ void add_atomically(u64* p, u64 v) {
+    atomicAdd(reinterpret_cast<unsigned long long*>(p), (unsigned long long)v);
+}
+__device__ __forceinline__ void add_atomically(ull2* p, ull2 v) {
+    add_atomically(reinterpret_cast<u64*>(p), v.x);
+    add_atomically(reinterpret_cast<u64*>(p) + 1, v.y);
+}
+
 // Gradient word by word: every token's row is added to its row of the table's gradient, a wave's atomics on 64 words in a row.
 // For few words that are added to a table, and where there is no scratch memory: 65536 tokens of 32000 x 1024: 833 us, 308
 // with scratch memory (two words a lane: 1670).
@@ -88,8 +96,8 @@ __global__ __launch_bounds__(THREADS) void embed_grad_kernel(const u64* __restri
     for (u64 i = (u64)blockIdx.x * THREADS + threadIdx.x; i < total; i += (u64)gridDim.x * THREADS) {
         const u64 j = i / D, c = i - j * D, id = (u64)(long long)ids[j];
         if (id >= V) continue;
-        atomicAdd(reinterpret_cast<unsigned long long*>(da + id * D + c), (unsigned long long)(ga[i] * alpha));
-        atomicAdd(reinterpret_cast<unsigned long long*>(db + id * D + c), (unsigned long long)(gb[i] * alpha));
+        add_atomically(da + id * D + c, ga[i] * alpha);
+        add_atomically(db + id * D + c, gb[i] * alpha);
     }
 }
 
@@ -161,7 +169,10 @@ __device__ __forceinline__ void count_in_table(const Id* __restrict__ ids, u64 n
         const u64 j = j0 + (u64)k * GROUP_THREADS;
         id[k] = j < n ? (u64)(long long)ids[j] : ~(u64)0;
     }
-    for (int i = threadIdx.x; i < TABLE; i += GROUP_THREADS) { key[i] = EMPTY; count[i] = 0; }
+    for (int i = threadIdx.x; i < TABLE / 4; i += GROUP_THREADS) {
+        reinterpret_cast<uint4*>(key)[i] = make_uint4(EMPTY, EMPTY, EMPTY, EMPTY);
+        reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+    }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < GROUP_TOKENS; ++k) {
@@ -205,9 +216,12 @@ __device__ __forceinline__ unsigned long long tokens_and_items(unsigned c, unsig
     return ((unsigned long long)((c + most - 1) / most) << 32) | c;
 }
 
-__device__ __forceinline__ void write_items(Item* items, unsigned row, unsigned first, unsigned c, unsigned most) {
-    const unsigned m = (c + most - 1) / most;
-    for (unsigned k = 0; k < m; ++k) items[k] = {row, first + k * most, k + 1 < m ? most : c - k * most, m == 1};
+// The items of a frequent row, by thread `mine` of `threads`.
+__device__ __forceinline__ void write_items(const Grouped& g, const Frequent& f, unsigned mine, unsigned threads) {
+    for (unsigned k = mine; k * g.most < f.count; k += threads) {
+        const unsigned left = f.count - k * g.most;
+        g.items[f.slot + k] = {f.row, f.first + k * g.most, left < g.most ? left : g.most, 0};
+    }
 }
 
 // The part of the n accesses at p that falls to this block, of all but the first.
@@ -233,28 +247,34 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_few_kernel(const Id* __re
         }
         return;
     }
-    __shared__ unsigned key[TABLE], count[TABLE];
+    __shared__ __align__(16) unsigned key[TABLE], count[TABLE];
+    __shared__ unsigned frequent_used;
     __shared__ unsigned long long wave_sum[GROUP_THREADS / 64];
+    __shared__ Frequent frequent[GROUP_THREADS * GROUP_TOKENS / 8];   // of more than 8 tokens each
     unsigned slot[GROUP_TOKENS], rank[GROUP_TOKENS];
     count_in_table(ids, n, V, threadIdx.x, key, count, slot, rank);
+    if (threadIdx.x == 0) frequent_used = 0;
     const int PLACES = TABLE / GROUP_THREADS;
-    const int p0 = threadIdx.x * PLACES;
     unsigned c[PLACES];
     unsigned long long own = 0, all;
 #pragma unroll
     for (int k = 0; k < PLACES; ++k) {
-        c[k] = count[p0 + k];
+        c[k] = count[threadIdx.x + k * GROUP_THREADS];
         own += tokens_and_items(c[k], g.most);
     }
     unsigned long long at = block_scan(own, wave_sum, &all);
 #pragma unroll
     for (int k = 0; k < PLACES; ++k) {
-        write_items(g.items + (at >> 32), key[p0 + k], (unsigned)at, c[k], g.most);
-        count[p0 + k] = (unsigned)at;
+        const int p = threadIdx.x + k * GROUP_THREADS;
+        if (c[k] > g.most) frequent[atomicAdd(&frequent_used, 1u)] = {key[p], (unsigned)at, c[k], (unsigned)(at >> 32)};
+        else if (c[k] > 0) g.items[at >> 32] = {key[p], (unsigned)at, c[k], 1};
+        count[p] = (unsigned)at;
         at += tokens_and_items(c[k], g.most);
     }
     if (threadIdx.x == 0) *g.cursor = all;
     __syncthreads();
+    for (unsigned i = threadIdx.x >> 6; i < frequent_used; i += GROUP_THREADS / 64)
+        write_items(g, frequent[i], threadIdx.x & 63, 64);
 #pragma unroll
     for (int k = 0; k < GROUP_TOKENS; ++k)
         if (slot[k] != EMPTY) g.list[count[slot[k]] + rank[k]] = threadIdx.x + k * GROUP_THREADS;
@@ -265,7 +285,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_few_kernel(const Id* __re
 // table, 10 with it).
 template <class Id>
 __global__ __launch_bounds__(GROUP_THREADS) void group_count_kernel(const Id* __restrict__ ids, u64 n, u64 V, Grouped g) {
-    __shared__ unsigned key[TABLE], count[TABLE];
+    __shared__ __align__(16) unsigned key[TABLE], count[TABLE];
     const u64 j0 = (u64)blockIdx.x * (GROUP_THREADS * GROUP_TOKENS) + threadIdx.x;
     unsigned slot[GROUP_TOKENS], rank[GROUP_TOKENS];
     count_in_table(ids, n, V, j0, key, count, slot, rank);
@@ -287,7 +307,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_offset_kernel(u64 V, Grou
     at += base;
     if (v < V) g.offset[v] = (unsigned)at;
     if (c > g.most) g.frequent[atomicAdd(g.frequent_used, 1u)] = {(unsigned)v, (unsigned)at, c, (unsigned)(at >> 32)};
-    else write_items(g.items + (at >> 32), (unsigned)v, (unsigned)at, c, g.most);
+    else if (c > 0) g.items[at >> 32] = {(unsigned)v, (unsigned)at, c, 1};
 }
 
 // The first token_blocks blocks fill the list; the others write down the items of frequent rows and clear the rows that those
@@ -305,10 +325,7 @@ __global__ __launch_bounds__(THREADS) void group_list_kernel(const Id* __restric
     const unsigned used = *g.frequent_used;
     for (unsigned i = blockIdx.x - token_blocks; i < used; i += gridDim.x - token_blocks) {
         const Frequent f = g.frequent[i];
-        for (unsigned k = threadIdx.x; k * g.most < f.count; k += THREADS) {
-            const unsigned left = f.count - k * g.most;
-            g.items[f.slot + k] = {f.row, f.first + k * g.most, left < g.most ? left : g.most, 0};
-        }
+        write_items(g, f, threadIdx.x, THREADS);
         if (accumulate) continue;
         for (u64 c = threadIdx.x; c < D; c += THREADS) {
             da[f.row * D + c] = 0;
@@ -373,14 +390,6 @@ struct RowSum {
         }
     }
 };
-
-__device__ __forceinline__ void add_atomically(u64* p, u64 v) {
-    atomicAdd(reinterpret_cast<unsigned long long*>(p), (unsigned long long)v);
-}
-__device__ __forceinline__ void add_atomically(ull2* p, ull2 v) {
-    add_atomically(reinterpret_cast<u64*>(p), v.x);
-    add_atomically(reinterpret_cast<u64*>(p) + 1, v.y);
-}
 
 // (65536 tokens of 32000 x 1024: 309 us with 4 accesses and 2 rows under way, 293 with 2 and 2, 288 with 2 and 8, 395 with 1 and 8)
 template <int W>

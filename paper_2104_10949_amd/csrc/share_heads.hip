@@ -306,7 +306,8 @@ cg_status cg_share_head_norm_rotate(const uint64_t* x_i, const uint64_t* x_ip1, 
     const u64 in_bytes[7] = {xbytes, xbytes, rbytes, rbytes, d->rot ? tbytes : 0, d->rot ? tbytes : 0,
                              d->rot ? (u64)d->rows * d->pos_bytes : 0};
     if (meets_inputs(z_i, zbytes, in, in_bytes, 7)) return CG_ERR_ALIAS;
-    const HeadParams p = head_params(x_i, x_ip1, r_i, r_ip1, cos, sin, pos, z_i, d);
+    HeadParams p = head_params(x_i, x_ip1, r_i, r_ip1, cos, sin, pos, z_i, d);
+    p.ld_g = 0;   // there is no g
     launch_rotate<false>(p, stream);
     return launched();
 }
