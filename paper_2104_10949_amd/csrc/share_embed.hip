@@ -225,27 +225,60 @@ __device__ __forceinline__ void write_items(const Grouped& g, const Frequent& f,
     }
 }
 
-// The part of the n accesses at p that falls to this block, of all but the first.
-template <class T>
-__device__ __forceinline__ void clear_stretch(T* p, u64 n) {
-    const u64 each = (n + gridDim.x - 2) / (gridDim.x - 1), begin = (blockIdx.x - 1) * each, end = begin + each < n ? begin + each : n;
-    for (u64 i = begin + threadIdx.x; i < end; i += GROUP_THREADS) __builtin_nontemporal_store(T(0), p + i);
+// Clears what `empty` says of `all` accesses to both components: this block's part of `blocks` blocks'.  A wave has `each` accesses
+// in a row, up to 32 KB of either component, before it goes on (522 MB in 117 us with a stretch of either component per
+// block, 99 with 8 KB in a row, 90 with 16 or 32).  `empty` is told where a row of accesses begins.
+template <class T, class Empty>
+__device__ __forceinline__ void clear_where(u64* da, u64* db, u64 all, unsigned each, unsigned block, unsigned blocks, const Empty& empty) {
+    const u64 waves = blockDim.x / 64;
+    T *pa = reinterpret_cast<T*>(da), *pb = reinterpret_cast<T*>(db);
+    for (u64 i0 = (block * waves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * each; i0 < all; i0 += blocks * waves * each) {
+        const auto is_empty = empty(i0);
+#pragma unroll 4
+        for (unsigned off = threadIdx.x & 63; off < each; off += 64) {
+            if (i0 + off < all && is_empty(off)) {
+                __builtin_nontemporal_store(T(0), pa + i0 + off);
+                __builtin_nontemporal_store(T(0), pb + i0 + off);
+            }
+        }
+    }
+}
+
+// ... the rows, of `units` accesses, of which `empty` holds.
+template <class T, class Empty>
+__device__ __forceinline__ void clear_rows(u64* da, u64* db, u64 V, unsigned units, unsigned each, unsigned block, unsigned blocks,
+                                           const Empty& empty) {
+    clear_where<T>(da, db, V * units, each, block, blocks, [&](u64 i0) {
+        const u64 row0 = i0 / units;
+        const unsigned c0 = (unsigned)(i0 - row0 * units);
+        return [=, &empty](unsigned off) { return empty(row0 + (c0 + off) / units); };
+    });
+}
+
+// How blocks of `threads` threads share out the clearing of so many accesses: as much in a row as leaves 4096 waves something,
+// a power of two of 64 accesses (393 MB in 68 us with 16 or 32 times 64, 81 with 23).
+struct Clearing {
+    unsigned each, blocks;
+};
+
+Clearing clearing_of(u64 accesses, unsigned threads, u64 most_blocks) {
+    Clearing c;
+    c.each = 64;
+    while (c.each < 32 * 64 && 2 * (u64)c.each * 4096 <= accesses) c.each *= 2;
+    const u64 per_block = (u64)(threads / 64) * c.each, blocks = (accesses + per_block - 1) / per_block;
+    c.blocks = (unsigned)(blocks < most_blocks ? blocks : most_blocks);
+    return c;
 }
 
 // Few tokens: the first block groups them all, while the others clear the gradient (no block is one that clears if it
 // is added to).  The rows with tokens are cleared, too: they are few where the table is large.
 template <class Id>
 __global__ __launch_bounds__(GROUP_THREADS) void group_few_kernel(const Id* __restrict__ ids, u64 n, u64 V, Grouped g,
-                                                                  u64* da, u64* db, u64 words, bool pairs) {
+                                                                  u64* da, u64* db, u64 words, bool pairs, unsigned clear_each) {
     if (blockIdx.x > 0) {
-        // a stretch of either component per block (75 -> 70 us for 393 MB against blocks that take turns)
-        if (pairs) {
-            clear_stretch(reinterpret_cast<ull2*>(da), words / 2);
-            clear_stretch(reinterpret_cast<ull2*>(db), words / 2);
-        } else {
-            clear_stretch(da, words);
-            clear_stretch(db, words);
-        }
+        const auto every = [](u64) { return [](unsigned) { return true; }; };
+        if (pairs) clear_where<ull2>(da, db, words / 2, clear_each, blockIdx.x - 1, gridDim.x - 1, every);
+        else clear_where<u64>(da, db, words, clear_each, blockIdx.x - 1, gridDim.x - 1, every);
         return;
     }
     __shared__ __align__(16) unsigned key[TABLE], count[TABLE];
@@ -396,39 +429,17 @@ struct RowSum {
 template <int W>
 using GroupSum = RowSum<W, 2, 8>;
 
-const int FILL_ACCESSES = 8;   // accesses per lane and component of a wave that clears: 8 KB in a row
-
-// Clears the rows of a table for which `empty` holds, in the order of the addresses: this block's part of `blocks` blocks'.
-template <int W, class Empty>
-__device__ __forceinline__ void clear_rows(u64* da, u64* db, u64 V, unsigned units, unsigned block, unsigned blocks, const Empty& empty) {
-    typedef typename Words<W>::type T;
-    const u64 all = V * units, chunk = FILL_ACCESSES * 64, waves = blockDim.x / 64;
-    T *pa = reinterpret_cast<T*>(da), *pb = reinterpret_cast<T*>(db);
-    for (u64 i0 = (block * waves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * chunk; i0 < all; i0 += blocks * waves * chunk) {
-        const u64 row0 = i0 / units;
-        const unsigned c0 = (unsigned)(i0 - row0 * units);
-#pragma unroll
-        for (int k = 0; k < FILL_ACCESSES; ++k) {
-            const unsigned off = k * 64 + (threadIdx.x & 63);
-            if (i0 + off < all && empty(row0 + (c0 + off) / units)) {
-                __builtin_nontemporal_store(T(0), pa + i0 + off);
-                __builtin_nontemporal_store(T(0), pb + i0 + off);
-            }
-        }
-    }
-}
-
 // The items, by blocks below item_blocks, the pieces of a row next to each other so that its memory is read in one go; the
 // other blocks clear the rows without tokens, in the order of the addresses.
 template <int W, bool WAVE>
 __global__ __launch_bounds__(THREADS) void group_sum_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb, u64 alpha,
                                                             u64* da, u64* db, u64 V, u64 D, int accumulate, int lg,
-                                                            unsigned pieces, unsigned item_blocks, Grouped g) {
+                                                            unsigned pieces, unsigned item_blocks, unsigned clear_each, Grouped g) {
     typedef typename Words<W>::type T;
     const int U = GroupSum<W>::U;
     const unsigned units = (unsigned)(D / W);
     if (blockIdx.x >= item_blocks) {
-        clear_rows<W>(da, db, V, units, blockIdx.x - item_blocks, gridDim.x - item_blocks, [&](u64 row) { return g.count[row] == 0; });
+        clear_rows<T>(da, db, V, units, clear_each, blockIdx.x - item_blocks, gridDim.x - item_blocks, [&](u64 row) { return g.count[row] == 0; });
         return;
     }
     const unsigned used = (unsigned)(*g.cursor >> 32);
@@ -511,7 +522,7 @@ template <class Id, int W>
 __global__ __launch_bounds__(FEW_THREADS) void few_sum_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
                                                               const Id* __restrict__ ids, u64 alpha, u64* da, u64* db, unsigned n,
                                                               u64 V, u64 D, unsigned pieces, unsigned pieces_each, unsigned shares,
-                                                              unsigned sum_blocks) {
+                                                              unsigned sum_blocks, unsigned clear_each) {
     typedef typename Words<W>::type T;
     typedef FewSum<W> Sum;
     const int U = Sum::U, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -529,7 +540,7 @@ __global__ __launch_bounds__(FEW_THREADS) void few_sum_kernel(const u64* __restr
             if (id < V) atomicOr(&lds.touched[id >> 5], 1u << (id & 31));
         }
         __syncthreads();
-        clear_rows<W>(da, db, V, units, blockIdx.x - sum_blocks, gridDim.x - sum_blocks,
+        clear_rows<T>(da, db, V, units, clear_each, blockIdx.x - sum_blocks, gridDim.x - sum_blocks,
                       [&](u64 row) { return !(lds.touched[row >> 5] >> (row & 31) & 1); });
         return;
     }
@@ -647,17 +658,17 @@ void launch_sum(const GradCall& c, const Grouped& g, hipStream_t s) {
     const int U = GroupSum<W>::U;
     const u64 units = c.D / W;
     const int lg = row_lanes_log2((units + U - 1) / U);
-    const u64 piece = (u64)U << lg, pieces = (units + piece - 1) / piece, per_fill = (u64)FILL_ACCESSES * THREADS;
-    u64 items = ((g.items_max * pieces << lg) + THREADS - 1) / THREADS, fills = c.accumulate || g.one_block ? 0 : (c.V * units + per_fill - 1) / per_fill;
+    const u64 piece = (u64)U << lg, pieces = (units + piece - 1) / piece;
+    u64 items = ((g.items_max * pieces << lg) + THREADS - 1) / THREADS;
     if (items > MAX_BLOCKS) items = MAX_BLOCKS;
-    if (fills > MAX_BLOCKS) fills = MAX_BLOCKS;
-    const dim3 grid((unsigned)(items + fills));
+    const Clearing clear = clearing_of(c.accumulate || g.one_block ? 0 : c.V * units, THREADS, MAX_BLOCKS);
+    const dim3 grid((unsigned)items + clear.blocks);
     if (lg == 6)
         hipLaunchKernelGGL((group_sum_kernel<W, true>), grid, dim3(THREADS), 0, s, c.ga, c.gb, c.alpha, c.da, c.db, c.V, c.D, c.accumulate, lg,
-                           (unsigned)pieces, (unsigned)items, g);
+                           (unsigned)pieces, (unsigned)items, clear.each, g);
     else
         hipLaunchKernelGGL((group_sum_kernel<W, false>), grid, dim3(THREADS), 0, s, c.ga, c.gb, c.alpha, c.da, c.db, c.V, c.D, c.accumulate, lg,
-                           (unsigned)pieces, (unsigned)items, g);
+                           (unsigned)pieces, (unsigned)items, clear.each, g);
 }
 
 // The way of a call, by its sizes.
@@ -679,11 +690,10 @@ void launch_few(const GradCall& c, hipStream_t s) {
     // a wave looks through the ids once for all pieces of its share of a row: as many as leave 8192 waves something to do
     u64 each = c.n * pieces / 8192;
     each = each < 1 ? 1 : each < pieces ? each : pieces;
-    const u64 shares = (pieces + each - 1) / each, sums = (c.n * shares + WAVES - 1) / WAVES, per_fill = (u64)FILL_ACCESSES * FEW_THREADS;
-    u64 fills = (c.V * units + per_fill - 1) / per_fill;
-    if (fills > 2048) fills = 2048;
-    hipLaunchKernelGGL((few_sum_kernel<Id, W>), dim3((unsigned)(sums + fills)), dim3(FEW_THREADS), 0, s, c.ga, c.gb, static_cast<const Id*>(c.ids),
-                       c.alpha, c.da, c.db, (unsigned)c.n, c.V, c.D, (unsigned)pieces, (unsigned)each, (unsigned)shares, (unsigned)sums);
+    const u64 shares = (pieces + each - 1) / each, sums = (c.n * shares + WAVES - 1) / WAVES;
+    const Clearing clear = clearing_of(c.V * units, FEW_THREADS, 2048);
+    hipLaunchKernelGGL((few_sum_kernel<Id, W>), dim3((unsigned)sums + clear.blocks), dim3(FEW_THREADS), 0, s, c.ga, c.gb, static_cast<const Id*>(c.ids),
+                       c.alpha, c.da, c.db, (unsigned)c.n, c.V, c.D, (unsigned)pieces, (unsigned)each, (unsigned)shares, (unsigned)sums, clear.each);
 }
 
 template <class Id>
@@ -692,10 +702,9 @@ void launch_grouped(const GradCall& c, bool vec, char* workspace, hipStream_t s)
     const Id* ids = static_cast<const Id*>(c.ids);
     const u64 words = c.V * c.D;
     if (g.one_block) {
-        u64 blocks = c.accumulate ? 0 : (words + 8 * GROUP_THREADS - 1) / (8 * GROUP_THREADS);
-        if (blocks > 2048) blocks = 2048;
         const bool pairs = aligned(c.da, 16) && aligned(c.db, 16) && words % 2 == 0;
-        hipLaunchKernelGGL(group_few_kernel<Id>, dim3(1 + (unsigned)blocks), dim3(GROUP_THREADS), 0, s, ids, c.n, c.V, g, c.da, c.db, words, pairs);
+        const Clearing clear = clearing_of(c.accumulate ? 0 : pairs ? words / 2 : words, GROUP_THREADS, 2048);
+        hipLaunchKernelGGL(group_few_kernel<Id>, dim3(1 + clear.blocks), dim3(GROUP_THREADS), 0, s, ids, c.n, c.V, g, c.da, c.db, words, pairs, clear.each);
         if (vec) launch_sum<2>(c, g, s);
         else launch_sum<1>(c, g, s);
         return;
