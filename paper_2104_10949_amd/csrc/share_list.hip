@@ -62,8 +62,8 @@ const int NORM_UNROLL = 8;   // loads of each component under way per lane
 // Clipping reads what the norm has read, as soon as the factor is there.  The norm's last KEEP_WORDS elements (both
 // components, 64 MB of the 256 MB that the memory-side cache holds) are therefore read as what is wanted again, and
 // clipping begins at the end; what lies before them streams past the caches, which is faster for the norm.  Norm of 25.5
-// million elements alone, norm and clipping of 19.3 million: 68, 53 and 102 us with all of it streaming, 68, 54 and 101 this way,
-// 74, 55 and 97 with 192 MB kept; with plain accesses and clipping from the beginning 82, 87 and 101.
+// million elements alone, norm and clipping of 19.3 million: 64, 52 and 103 us this way, 68, 52 and 102 with 128 MB kept, 71, 53 and
+// 96 with 192 MB; with plain accesses and clipping from the beginning 82, 87 and 101.
 const u64 KEEP_WORDS = (u64)4 << 20;
 
 template <bool KEEP>
@@ -236,10 +236,11 @@ cg_status check_list(const u64* const* const* lists, int parts, const size_t* n,
     return CG_OK;
 }
 
-// Words of a block's chunk: about `blocks` blocks together, and no less than what keeps one busy.
+// Words of a block's chunk: a power of two, at least `least` and as many as leave at most `blocks` blocks (and one per tensor).
 u64 chunk_words(u64 total, u64 blocks, u64 least) {
-    const u64 c = (total / blocks + 1023) / 1024 * 1024;
-    return c < least ? least : c;
+    u64 c = least;
+    while (c * blocks < total) c *= 2;
+    return c;
 }
 
 }  // namespace
@@ -256,7 +257,7 @@ cg_status cg_share_sq_norm(const uint64_t* const* x_i, const uint64_t* const* x_
     for (size_t k = 0; k < count; ++k)
         if (n[k] > 0 && (cg::overlap(z_i, 8, x_i[k], n[k] * 8) || cg::overlap(z_i, 8, x_ip1[k], n[k] * 8))) return CG_ERR_ALIAS;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const u64 chunk = chunk_words(total, 1024, NORM_UNROLL * NORM_THREADS);
+    const u64 chunk = chunk_words(total, 2048, NORM_UNROLL * NORM_THREADS);
     // up to four chunks, a round trip to memory each, are less than a launch that clears the word
     u64 chunks = 0;
     for (size_t k = 0; k < count && chunks <= 4; ++k) chunks += (n[k] + chunk - 1) / chunk;
@@ -311,7 +312,7 @@ cg_status cg_share_clip(const uint64_t* const* xa, const uint64_t* const* xb, co
     if (total == 0) return CG_OK;
     if (cg_status st = check_written(lists, n, count)) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const u64 chunk = chunk_words(total, 16384, 1024);
+    const u64 chunk = chunk_words(total, 1 << 22, 1024);
     u64 done = 0;   // words of tensor k behind here
     for (size_t next = count; next > 0;) {
         ClipArgs t;
