@@ -120,31 +120,49 @@ struct Grouped {   // in the scratch memory
     unsigned long long* cursor;   // tokens placed so far, and items in the upper half; starts at zero, as frequent_used and the counts do
     unsigned *frequent_used, *count, *offset, *rank, *list;
     Frequent* frequent;
+    unsigned char* touched;       // of a middling call instead of all that but the list: a bit per row with tokens
     Item* items;
     u64 items_max, bytes;
     unsigned most;      // tokens of an item, at most 64
-    bool one_block;     // the tokens are few enough for one block's LDS: no counts, offsets and ranks in memory
+    unsigned buckets;   // of a middling call, a power of two
+    bool middling;      // one launch groups
+    bool clear_first;   // ... and clears the whole table by the way
 };
 
-const int GROUP_THREADS = 1024, GROUP_TOKENS = 4;   // of a block that groups, and of each of its threads
+const int GROUP_THREADS = 1024, GROUP_TOKENS = 4;   // of a block that counts tokens, and of each of its threads
 const int TABLE = 2 * GROUP_THREADS * GROUP_TOKENS; // places of its hash table: at most half full
 const unsigned EMPTY = ~0u;                         // no row: V < 2^31
 
+// Middling calls: every block of `buckets` looks through all ids for those of its own rows, eight in a row and every
+// buckets-th eight, and groups them in LDS.  Two launches instead of five; above 20480 tokens the looking through takes longer than
+// the launches, and the sums like neighbouring rows better (18485 tokens of 27825 x 16: 29 us and 33 with three launches more;
+// 32768 of 32000 x 768: 184 and 172; 65536 of 32000 x 1024: 356 and 311).
+const unsigned MIDDLING = 20480, BUCKETS = 128;   // most tokens, most buckets
+const u64 MIDDLING_ROWS = (u64)BUCKETS * 8 * GROUP_THREADS;
+
 Grouped grouped_layout(char* p, u64 n, u64 V, u64 D) {
     Grouped g = {};
-    // a wave takes two microseconds for four tokens: items short enough for 8192 waves of 256 words, and in a large call
+    // a wave takes two microseconds for eight tokens: items short enough for 8192 waves of 256 words, and in a large call
     // long enough to need few atomics (63904 tokens of 320 x 105: 53 us with 4 tokens, 36 with 8, 29 with 16, 58 with 64)
-    g.one_block = n <= GROUP_THREADS * GROUP_TOKENS;
-    const unsigned least = g.one_block ? 8 : 16;
+    g.middling = n <= MIDDLING && V <= MIDDLING_ROWS;
+    // a row with tokens is then written twice, but its clearing is hidden, and writes go faster without reads among them (4096 tokens of
+    // 32000 x 768: 84 us, 87 with the rows without tokens cleared by the sums' launch; 2000 of 128000 x 255: 96 and 109)
+    g.clear_first = g.middling && n * D <= 6000000 + V * D / 5;
+    g.buckets = 32;   // (16 to 64 are alike; 128 keep the clearing waiting, 5 us of 68)
+    while (g.buckets < BUCKETS && (u64)g.buckets * 8 * GROUP_THREADS < V) g.buckets *= 2;
+    const unsigned least = n <= 4096 ? 8 : 16;
     const double most = (double)n * (double)D / (256.0 * 8192.0);
     g.most = most < least ? least : most < 64 ? (unsigned)most : 64;
-    g.items_max = (n < V ? n : V) + 2 * n / g.most;   // rows with tokens; of those with c > most, ceil(c / most) items each
+    // middling: as many places as tokens, some of them left empty; else rows with tokens, of those with c > most ceil(c / most) items each
+    g.items_max = g.middling ? n : (n < V ? n : V) + 2 * n / g.most;
     u64 at = 0;
     const auto take = [&](u64 bytes) { char* q = p + at; at += (bytes + 255) / 256 * 256; return q; };
-    g.cursor = reinterpret_cast<unsigned long long*>(take(12 + (g.one_block ? 0 : V * 4)));
+    g.cursor = reinterpret_cast<unsigned long long*>(take(12 + (g.middling ? 0 : V * 4)));
     g.frequent_used = reinterpret_cast<unsigned*>(g.cursor + 1);
     g.count = g.frequent_used + 1;
-    if (!g.one_block) {
+    if (g.middling) {
+        g.touched = reinterpret_cast<unsigned char*>(take((V + 7) / 8));
+    } else {
         g.frequent = reinterpret_cast<Frequent*>(take(n / g.most * sizeof(Frequent)));
         g.offset = reinterpret_cast<unsigned*>(take(V * 4));
         g.rank = reinterpret_cast<unsigned*>(take(n * 4));
@@ -270,48 +288,101 @@ Clearing clearing_of(u64 accesses, unsigned threads, u64 most_blocks) {
     return c;
 }
 
-// Few tokens: the first block groups them all, while the others clear the gradient (no block is one that clears if it
-// is added to).  The rows with tokens are cleared, too: they are few where the table is large.
+// A middling call's grouping.  Nothing has to be zero before, and the blocks need nothing of each other: a block that sees all
+// ids knows how many tokens the buckets before its own have, which is where its part of the list and of the items begins
+// (an item has a token at least).  It also clears its frequent rows, or blocks behind the buckets' clear the whole table.
 template <class Id>
-__global__ __launch_bounds__(GROUP_THREADS) void group_few_kernel(const Id* __restrict__ ids, u64 n, u64 V, Grouped g,
-                                                                  u64* da, u64* db, u64 words, bool pairs, unsigned clear_each) {
-    if (blockIdx.x > 0) {
+__global__ __launch_bounds__(GROUP_THREADS) void group_buckets_kernel(const Id* __restrict__ ids, unsigned n, u64 V, u64 D, int accumulate,
+                                                                      u64* da, u64* db, bool pairs, unsigned clear_each, Grouped g) {
+    if (blockIdx.x >= g.buckets) {
         const auto every = [](u64) { return [](unsigned) { return true; }; };
-        if (pairs) clear_where<ull2>(da, db, words / 2, clear_each, blockIdx.x - 1, gridDim.x - 1, every);
-        else clear_where<u64>(da, db, words, clear_each, blockIdx.x - 1, gridDim.x - 1, every);
+        if (pairs) clear_where<ull2>(da, db, V * D / 2, clear_each, blockIdx.x - g.buckets, gridDim.x - g.buckets, every);
+        else clear_where<u64>(da, db, V * D, clear_each, blockIdx.x - g.buckets, gridDim.x - g.buckets, every);
         return;
     }
-    __shared__ __align__(16) unsigned key[TABLE], count[TABLE];
-    __shared__ unsigned frequent_used;
+    const int UNROLLED = 8;
+    __shared__ __align__(16) unsigned count[8 * GROUP_THREADS];
     __shared__ unsigned long long wave_sum[GROUP_THREADS / 64];
-    __shared__ Frequent frequent[GROUP_THREADS * GROUP_TOKENS / 8];   // of more than 8 tokens each
-    unsigned slot[GROUP_TOKENS], rank[GROUP_TOKENS];
-    count_in_table(ids, n, V, threadIdx.x, key, count, slot, rank);
-    if (threadIdx.x == 0) frequent_used = 0;
-    const int PLACES = TABLE / GROUP_THREADS;
-    unsigned c[PLACES];
-    unsigned long long own = 0, all;
+    __shared__ uint2 frequent[MIDDLING / 16];   // rows of more than 16 tokens each, or of more than 8 of at most 4096 tokens: place and count, first item
+    __shared__ unsigned frequent_used, before, valid;
+    const int shift = __builtin_ctz(g.buckets);
+    const unsigned b = blockIdx.x, groups = (unsigned)((V + 7) / 8), own_groups = groups > b ? (groups - b - 1) / g.buckets + 1 : 0;
+    for (unsigned i = threadIdx.x; i < 2 * own_groups; i += GROUP_THREADS) reinterpret_cast<uint4*>(count)[i] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x == 0) frequent_used = before = valid = 0;
+    __syncthreads();
+    // calls f(token, place of its row in `count`) for the tokens of the own rows, and g(bucket) for every valid one
+    const auto look_through = [&](const auto& own, const auto& any) {
+        for (unsigned j0 = threadIdx.x; j0 < n; j0 += UNROLLED * GROUP_THREADS) {
+            u64 id[UNROLLED];
 #pragma unroll
-    for (int k = 0; k < PLACES; ++k) {
-        c[k] = count[threadIdx.x + k * GROUP_THREADS];
+            for (int k = 0; k < UNROLLED; ++k) {
+                const unsigned j = j0 + k * GROUP_THREADS;
+                id[k] = j < n ? (u64)(long long)ids[j] : ~(u64)0;
+            }
+#pragma unroll
+            for (int k = 0; k < UNROLLED; ++k) {
+                if (id[k] >= V) continue;
+                const unsigned group = (unsigned)id[k] >> 3, bucket = group & (g.buckets - 1);
+                any(bucket);
+                if (bucket == b) own(j0 + k * GROUP_THREADS, (group >> shift) * 8 + ((unsigned)id[k] & 7));
+            }
+        }
+    };
+    unsigned smaller = 0, all_valid = 0;
+    look_through([&](unsigned, unsigned place) { atomicAdd(&count[place], 1u); },
+                 [&](unsigned bucket) { smaller += bucket < b; ++all_valid; });
+    for (int h = 32; h > 0; h >>= 1) {
+        smaller += __shfl_xor(smaller, h);
+        all_valid += __shfl_xor(all_valid, h);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        atomicAdd(&before, smaller);
+        atomicAdd(&valid, all_valid);
+    }
+    __syncthreads();
+    // a thread has eight rows
+    unsigned c[8];
+    unsigned long long own = 0, all;
+    unsigned touched = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        c[k] = threadIdx.x < own_groups ? count[8 * threadIdx.x + k] : 0;
         own += tokens_and_items(c[k], g.most);
+        touched |= (c[k] > 0 ? 1u : 0u) << k;
     }
     unsigned long long at = block_scan(own, wave_sum, &all);
+    Item* items = g.items + before;
+    unsigned* list = g.list + before;
+    if (threadIdx.x < own_groups) {
+        const unsigned group = threadIdx.x * g.buckets + b;
+        g.touched[group] = (unsigned char)touched;
 #pragma unroll
-    for (int k = 0; k < PLACES; ++k) {
-        const int p = threadIdx.x + k * GROUP_THREADS;
-        if (c[k] > g.most) frequent[atomicAdd(&frequent_used, 1u)] = {key[p], (unsigned)at, c[k], (unsigned)(at >> 32)};
-        else if (c[k] > 0) g.items[at >> 32] = {key[p], (unsigned)at, c[k], 1};
-        count[p] = (unsigned)at;
-        at += tokens_and_items(c[k], g.most);
+        for (int k = 0; k < 8; ++k) {
+            const unsigned row = 8 * group + k, first = (unsigned)at, slot = (unsigned)(at >> 32);
+            if (c[k] > g.most) frequent[atomicAdd(&frequent_used, 1u)] = make_uint2((8 * threadIdx.x + k) | c[k] << 13, slot);
+            else if (c[k] > 0) items[slot] = {row, before + first, c[k], 1};
+            count[8 * threadIdx.x + k] = first;
+            at += tokens_and_items(c[k], g.most);
+        }
     }
-    if (threadIdx.x == 0) *g.cursor = all;
+    for (unsigned i = (unsigned)(all >> 32) + threadIdx.x; i < (unsigned)all; i += GROUP_THREADS) items[i] = {0, 0, 0, 1};
+    if (b == 0 && threadIdx.x == 0) *g.cursor = (unsigned long long)valid << 32;
     __syncthreads();
-    for (unsigned i = threadIdx.x >> 6; i < frequent_used; i += GROUP_THREADS / 64)
-        write_items(g, frequent[i], threadIdx.x & 63, 64);
-#pragma unroll
-    for (int k = 0; k < GROUP_TOKENS; ++k)
-        if (slot[k] != EMPTY) g.list[count[slot[k]] + rank[k]] = threadIdx.x + k * GROUP_THREADS;
+    for (unsigned i = threadIdx.x >> 6; i < frequent_used; i += GROUP_THREADS / 64) {
+        const unsigned lane = threadIdx.x & 63, place = frequent[i].x & 8191, tokens = frequent[i].x >> 13;
+        const unsigned row = 8 * ((place >> 3 << shift) + b) + (place & 7), first = before + count[place];
+        for (unsigned k = lane; k * g.most < tokens; k += 64) {
+            const unsigned left = tokens - k * g.most;
+            items[frequent[i].y + k] = {row, first + k * g.most, left < g.most ? left : g.most, 0};
+        }
+        if (accumulate || g.clear_first) continue;
+        for (u64 e = lane; e < D; e += 64) {
+            da[row * D + e] = 0;
+            db[row * D + e] = 0;
+        }
+    }
+    __syncthreads();   // the counts are read above and go up below
+    look_through([&](unsigned j, unsigned place) { list[atomicAdd(&count[place], 1u)] = j; }, [](unsigned) {});
 }
 
 // rank[j] = how many tokens of the same id came before.  A block adds one number per id to the row's count: atomics of
@@ -439,7 +510,9 @@ __global__ __launch_bounds__(THREADS) void group_sum_kernel(const u64* __restric
     const int U = GroupSum<W>::U;
     const unsigned units = (unsigned)(D / W);
     if (blockIdx.x >= item_blocks) {
-        clear_rows<T>(da, db, V, units, clear_each, blockIdx.x - item_blocks, gridDim.x - item_blocks, [&](u64 row) { return g.count[row] == 0; });
+        const unsigned block = blockIdx.x - item_blocks, blocks = gridDim.x - item_blocks;
+        if (g.middling) clear_rows<T>(da, db, V, units, clear_each, block, blocks, [&](u64 row) { return !(g.touched[row >> 3] >> (row & 7) & 1); });
+        else clear_rows<T>(da, db, V, units, clear_each, block, blocks, [&](u64 row) { return g.count[row] == 0; });
         return;
     }
     const unsigned used = (unsigned)(*g.cursor >> 32);
@@ -455,6 +528,7 @@ __global__ __launch_bounds__(THREADS) void group_sum_kernel(const u64* __restric
             if (c[u] >= units) c[u] = units - 1;
         }
         const Item it = g.items[index];
+        if (it.count == 0) continue;   // a place left empty
         GroupSum<W> sum;
         sum.clear();
         if (WAVE) {
@@ -661,7 +735,7 @@ void launch_sum(const GradCall& c, const Grouped& g, hipStream_t s) {
     const u64 piece = (u64)U << lg, pieces = (units + piece - 1) / piece;
     u64 items = ((g.items_max * pieces << lg) + THREADS - 1) / THREADS;
     if (items > MAX_BLOCKS) items = MAX_BLOCKS;
-    const Clearing clear = clearing_of(c.accumulate || g.one_block ? 0 : c.V * units, THREADS, MAX_BLOCKS);
+    const Clearing clear = clearing_of(c.accumulate || g.clear_first ? 0 : c.V * units, THREADS, MAX_BLOCKS);
     const dim3 grid((unsigned)items + clear.blocks);
     if (lg == 6)
         hipLaunchKernelGGL((group_sum_kernel<W, true>), grid, dim3(THREADS), 0, s, c.ga, c.gb, c.alpha, c.da, c.db, c.V, c.D, c.accumulate, lg,
@@ -700,11 +774,12 @@ template <class Id>
 void launch_grouped(const GradCall& c, bool vec, char* workspace, hipStream_t s) {
     const Grouped g = grouped_layout(workspace, c.n, c.V, c.D);
     const Id* ids = static_cast<const Id*>(c.ids);
-    const u64 words = c.V * c.D;
-    if (g.one_block) {
+    if (g.middling) {
+        const u64 words = c.V * c.D;
         const bool pairs = aligned(c.da, 16) && aligned(c.db, 16) && words % 2 == 0;
-        const Clearing clear = clearing_of(c.accumulate ? 0 : pairs ? words / 2 : words, GROUP_THREADS, 2048);
-        hipLaunchKernelGGL(group_few_kernel<Id>, dim3(1 + clear.blocks), dim3(GROUP_THREADS), 0, s, ids, c.n, c.V, g, c.da, c.db, words, pairs, clear.each);
+        const Clearing clear = clearing_of(c.accumulate || !g.clear_first ? 0 : pairs ? words / 2 : words, GROUP_THREADS, 2048);
+        hipLaunchKernelGGL(group_buckets_kernel<Id>, dim3(g.buckets + clear.blocks), dim3(GROUP_THREADS), 0, s, ids, (unsigned)c.n, c.V, c.D,
+                           c.accumulate, c.da, c.db, pairs, clear.each, g);
         if (vec) launch_sum<2>(c, g, s);
         else launch_sum<1>(c, g, s);
         return;

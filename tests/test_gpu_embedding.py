@@ -39,6 +39,8 @@ def draw_ids(kind, n, V, seed):
         return np.full(n, -1, np.int64)
     if kind == "rank":                                   # frequencies as of words: the first id half of the time
         return (np.exp(rng.random(n) * np.log(V + 1)) - 1).astype(np.int64).clip(0, V - 1)
+    if kind == "bucket":                                 # rows that the same block looks after
+        return (rng.integers(0, 8, n) + rng.integers(0, max(1, V // 1024), n) * 1024).clip(0, V - 1)
     if kind == "position":
         return np.arange(n) % V
     ids = rng.integers(0, V, n)
@@ -118,12 +120,12 @@ def test_lookup_beyond_32_bit_offsets(cg):
 
 
 # (n, V, D): one token to many, rows shorter and longer than a wave's piece, tables smaller and larger than the batch
-GRADS = [(1, 1, 1), (1, 700, 512), (2, 5, 3), (63, 7, 16), (64, 64, 64), (65, 1000, 30), (128, 300, 514), (129, 300, 514), (100, 40, 1031), (500, 3, 515), (777, 1531, 130), (1024, 2000, 257), (1025, 100, 260), (1024, 3, 70000), (600, (1 << 18) + 5, 4), (600, 1 << 18, 4), (2048, 60, 512), (2048, 60, 513), (2049, 60, 8), (2048, 100, 258),
+GRADS = [(1, 1, 1), (1, 700, 512), (2, 5, 3), (63, 7, 16), (64, 64, 64), (65, 1000, 30), (128, 300, 514), (129, 300, 514), (100, 40, 1031), (500, 3, 515), (777, 1531, 130), (1024, 2000, 257), (1025, 100, 260), (1024, 3, 70000), (600, (1 << 18) + 5, 4), (600, 1 << 18, 4), (2048, 60, 512), (2048, 60, 513), (2049, 60, 8), (4096, 9, 40), (20480, 1200, 6), (20481, 1200, 6), (20480, 300, 9), (20480, 1000, 700), (5000, 1 << 20, 2), (5000, (1 << 20) + 1, 2), (9000, 130 * 1024, 5), (2048, 100, 258),
          (4096, 300, 8), (4097, 40, 64), (5000, 5000, 20), (3000, 9, 1030), (9001, 2000, 33), (20000, 700, 34), (16384, 16384, 6), (40000, 50, 18)]
 
 
 @pytest.mark.parametrize("n,V,D", GRADS)
-@pytest.mark.parametrize("kind", ["rank", "mixed", "one", "position"])
+@pytest.mark.parametrize("kind", ["rank", "mixed", "one", "position", "bucket"])
 @pytest.mark.parametrize("scratch", [True, False])
 def test_gradient(cg, ro, wl, n, V, D, kind, scratch):
     say(f"gradient n={n} V={V} D={D} {kind}, scratch memory {scratch}")
