@@ -87,7 +87,7 @@ __device__ __forceinline__ void add_atomically(ull2* p, ull2 v) {
 }
 
 // Gradient word by word: every token's row is added to its row of the table's gradient, a wave's atomics on 64 words in a row.
-// For few words that are added to a table, and where there is no scratch memory: 65536 tokens of 32000 x 1024: 833 us, 308
+// For few words that are added to a table, and where there is no scratch memory: 65536 tokens of 32000 x 1024: 833 us, 304
 // with scratch memory (two words a lane: 1670).
 template <class Id>
 __global__ __launch_bounds__(THREADS) void embed_grad_kernel(const u64* __restrict__ ga, const u64* __restrict__ gb,
