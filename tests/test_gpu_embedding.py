@@ -147,7 +147,7 @@ def test_gradient(cg, ro, wl, n, V, D, kind, scratch):
     assert bool((memory[:256] == 0x5A).all()) and bool((memory[256 + need:] == 0x5A).all())
 
 
-@pytest.mark.parametrize("n", [0, 40, 5000, 20000])
+@pytest.mark.parametrize("n", [0, 40, 5000, 20000, 30000])
 def test_gradient_of_padding_alone(cg, wl, n):
     say(f"gradient of {n} tokens of padding")
     V, D = 31, 22
@@ -161,7 +161,7 @@ def test_gradient_of_padding_alone(cg, wl, n):
     assert all(not t.host().any() for t in d)
 
 
-@pytest.mark.parametrize("n", [300, 3000, 20000])
+@pytest.mark.parametrize("n", [300, 3000, 20000, 30000])
 def test_gradient_on_another_stream_and_of_changing_ids(cg, ro, wl, n):
     """Calls one after the other on one stream with ids and gradients overwritten in between, each checked."""
     say(f"gradient on a stream of its own, n={n}")
@@ -186,7 +186,7 @@ def test_gradient_on_another_stream_and_of_changing_ids(cg, ro, wl, n):
             assert np.array_equal(cg.to_host(a), w), first_mismatch(cg.to_host(a), w)
 
 
-@pytest.mark.parametrize("n", [500, 3000, 20000])
+@pytest.mark.parametrize("n", [500, 3000, 20000, 30000])
 def test_gradients_on_two_streams_at_once(cg, ro, wl, n):
     """Calls under way at the same time on two streams, scratch memory from the allocator for each."""
     say(f"two gradients of {n} tokens at once")
@@ -210,7 +210,7 @@ def test_gradients_on_two_streams_at_once(cg, ro, wl, n):
                 assert np.array_equal(cg.to_host(a), w), first_mismatch(cg.to_host(a), w)
 
 
-@pytest.mark.parametrize("n", [300, 3000, 20000])
+@pytest.mark.parametrize("n", [300, 3000, 20000, 30000])
 def test_gradient_in_two_graphs(cg, ro, wl, n):
     """Two captured calls, replayed in turn with new inputs and the program's own work in between."""
     say(f"gradient in two graphs, n={n}")
