@@ -707,7 +707,7 @@ def cg_share_embedding_grad(ga, gb, ids, V: int, alpha: int = 1, da=None, db=Non
     ip, width = _index_ptr(ids)
     n = ids.numel()
     if workspace is None:
-        workspace = _scratch(lib().cg_share_embedding_grad_workspace_bytes(n, V, D, accumulate), ga.device, stream)
+        workspace = _scratch(lib().cg_share_embedding_grad_workspace_bytes(n, V, D, bool(accumulate)), ga.device, stream)
     else:
         _current(workspace)
     wp, wb = _ws(workspace)

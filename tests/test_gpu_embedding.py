@@ -210,6 +210,16 @@ def test_gradients_on_two_streams_at_once(cg, ro, wl, n):
                 assert np.array_equal(cg.to_host(a), w), first_mismatch(cg.to_host(a), w)
 
 
+def test_gradient_added_as_a_numpy_truth_value_says(cg, ro, wl):
+    n, V, D = 5000, 60, 12
+    host = draw_ids("uniform", n, V, 3)
+    ids, G = torch.from_numpy(host).cuda(), [wl.draw_ring((n, D), 230 + c) for c in range(2)]
+    g, d = [cg.to_device(h) for h in G], [torch.ones((V, D), dtype=torch.int64, device="cuda") for _ in range(2)]
+    cg.cg_share_embedding_grad(*g, ids, V, da=d[0], db=d[1], accumulate=np.bool_(True))
+    for t, h in zip(d, G):
+        assert np.array_equal(cg.to_host(t), ro.embedding_grad(h, host, V, 1) + np.uint64(1))
+
+
 @pytest.mark.parametrize("n", [300, 3000, 20000, 30000])
 def test_gradient_in_two_graphs(cg, ro, wl, n):
     """Two captured calls, replayed in turn with new inputs and the program's own work in between."""
