@@ -730,12 +730,13 @@ def _row_step(t: torch.Tensor) -> int:
 
 
 def _pair_step(a: torch.Tensor, b: torch.Tensor, shape) -> int:
-    """... of both components."""
+    """... of both components.  Their strides may differ where a dimension has one entry and its stride says nothing."""
     if a.shape != shape or b.shape != shape or len(shape) != 3:
         raise ValueError("heads must be [rows, heads, dim] tensors of one shape")
-    if a.stride() != b.stride():
+    step = _row_step(a)
+    if b is not a and _row_step(b) != step:
         raise ValueError("both components must have their rows equally far apart")
-    return _row_step(a)
+    return step
 
 
 def _ring_ptrs(*tensors) -> list:
