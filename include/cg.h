@@ -640,7 +640,7 @@ CG_API size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t
  *              between the rows is left alone).  r, dr and the sums are contiguous.
  *
  * Results are additive shares at the product's scale (x, r and the angles' bits together), not re-shared, not
- * truncated.  CG_ERR_SHAPE for a dimension that does not fit the above, CG_ERR_UNSUPPORTED if
+ * truncated; a party blinds them (cg_reshare) before it sends them.  CG_ERR_SHAPE for a dimension that does not fit the above, CG_ERR_UNSUPPORTED if
  * rows*heads exceeds 2^31-1.  Outputs must not overlap inputs or each other, from the first word to
  * the last (CG_ERR_ALIAS).  rows == 0 returns CG_OK.
  */
@@ -666,10 +666,13 @@ CG_API cg_status cg_share_head_norm_rotate_grad(const uint64_t *g_i, const uint6
  *
  *   cg_share_sq_norm : z_i = sum over all elements of all tensors of x_i x_i + x_{i+1} x_i + x_i x_{i+1}:
  *                      the party's additive share (one word) of the squared global norm, with twice
- *                      the gradients' fractional bits
- *   cg_clip_factor   : the public factor once the three shares s0, s1, s2 (device words) have been opened
- *                      to each other: with S = s0 + s1 + s2 read as unsigned and N = floor(sqrt(S))
- *                      (the norm, at the gradients' scale; max_norm is a word of that scale, too),
+ *                      the gradients' fractional bits.  It is a product like any other: a party
+ *                      blinds it with a zero share (cg_reshare) before it sends it, else the word
+ *                      tells the receiver about the share that it does not hold.
+ *   cg_clip_factor   : the public factor, from s0, s1, s2: the three parties' blinded words (device
+ *                      words), opened to each other: with S = s0 + s1 + s2 read as unsigned and
+ *                      N = floor(sqrt(S)) (the norm, at the gradients' scale; max_norm is a word of
+ *                      that scale, too),
  *                        factor = 2^frac_bits                          if N <= max_norm
  *                                 floor(max_norm * 2^frac_bits / N)    otherwise.
  *                      In integers, so that the parties get the same word.  factor may be one of
