@@ -619,7 +619,8 @@ CG_API size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t
  * (ld_x >= heads*dim words from a row to the next, e.g. the packed output of their projection).
  *
  *   cg_share_head_sq_sum      : z_i[t,h] = sum_d x_i x_i + x_{i+1} x_i + x_i x_{i+1}: the party's additive
- *                               share of the head's sum of squares, [rows, heads]
+ *                               share of the head's sum of squares, [rows, heads], which it is only while
+ *                               that sum is below 2^64
  *   cg_share_head_norm_rotate : u = three-term product of x[t,h,:] with the shared word r[t,h] (the
  *                               inverse norm, [rows, heads]); z_i[t,h,:] = u turned by the public angles
  *                               of position pos[t]: for pair p < rot/2 of the first `rot` elements, with
@@ -675,7 +676,13 @@ CG_API cg_status cg_share_head_norm_rotate_grad(const uint64_t *g_i, const uint6
  *                      that scale, too),
  *                        factor = 2^frac_bits                          if N <= max_norm
  *                                 floor(max_norm * 2^frac_bits / N)    otherwise.
- *                      In integers, so that the parties get the same word.  factor may be one of
+ *                      In integers, so that the parties get the same word.  S is the squared norm only
+ *                      while that is below 2^64, that is, N below 2^32: a real norm below 2^(32-f) at f
+ *                      fractional bits (65536 at 16).  A larger one wraps to any S, and the gradients
+ *                      may pass unclipped with nothing to tell it by: a program whose gradients may
+ *                      grow so far takes the norm of gradients with fewer fractional bits (the
+ *                      protocol's truncation, cg_trunc1_local, before cg_share_sq_norm).  A max_norm of
+ *                      2^32 or more is never exceeded.  factor may be one of
  *                      s0, s1, s2.  CG_ERR_SHAPE unless 0 <= frac_bits <= 62 and max_norm * 2^frac_bits
  *                      < 2^64.  (Opening the norm tells it to the parties.  A program that must not
  *                      keeps the factor shared and multiplies with cg_share_mul, period 1.)

@@ -848,7 +848,7 @@ class ShareList:
 
 def cg_share_sq_norm(x: ShareList, z_i=None, stream=None) -> torch.Tensor:
     """z_i [1]: the party's additive share of the squared norm over all tensors of the list; to be blinded (cg_reshare) before it
-    is sent to anyone."""
+    is sent to anyone.  Mod 2^64: right for a norm below 2^32 at the gradients' scale (65536 at 16 fractional bits)."""
     if z_i is None:
         z_i = torch.empty((1,), dtype=torch.int64, device=x.a[0].device if x.count else "cuda")
     elif z_i.numel() != 1:
@@ -860,7 +860,8 @@ def cg_share_sq_norm(x: ShareList, z_i=None, stream=None) -> torch.Tensor:
 
 def cg_clip_factor(s0, s1, s2, max_norm: int, frac_bits: int, factor=None, stream=None) -> torch.Tensor:
     """factor [1]: 2^frac_bits, or that times max_norm / norm rounded down where the norm, the root of the opened sum s0 + s1 + s2
-    of the parties' blinded words, is larger; max_norm is a fixed-point word of the gradients' scale."""
+    of the parties' blinded words, is larger; max_norm is a fixed-point word of the gradients' scale.  A norm
+    of 2^32 or more at that scale has wrapped and may pass unclipped."""
     factor = s0.new_empty((1,)) if factor is None else factor
     if any(t.numel() != 1 for t in (s0, s1, s2, factor)):
         raise ValueError("the shares of the squared norm and the factor are one word each")

@@ -33,3 +33,28 @@ def test_the_header_says_that_shares_are_blinded_before_they_are_sent():
     text = header()
     assert "blinds it with a zero share (cg_reshare) before it sends it" in text
     assert "s0, s1, s2: the three parties' blinded words" in text
+
+
+def norm_of(x):
+    """The opened sum of squares of plain words, by way of three parties' shares."""
+    s = ro.share(x, wl.draw_ring(x.shape, 710), wl.draw_ring(x.shape, 711))
+    return sum(ro.sq_norm([(s[i], s[(i + 1) % 3])]) for i in range(3)) % MOD
+
+
+def test_the_norm_is_right_below_2_to_the_32_and_wraps_from_there():
+    """At 16 fractional bits: a norm of 65536 - 2^-16 is clipped, one of 65536 is taken for zero; no bound of 2^32 or more clips."""
+    largest = np.array([(1 << 32) - 1], np.uint64)
+    assert norm_of(largest) == ((1 << 32) - 1) ** 2
+    assert ro.clip_factor(norm_of(largest), 1 << 16, 16) == 1
+    beyond = np.array([1 << 32], np.uint64)
+    assert norm_of(beyond) == 0 and ro.clip_factor(norm_of(beyond), 1 << 16, 16) == 1 << 16
+    several = np.array([1 << 31] * 4 + [-(1 << 31) % MOD] * 3 + [3], np.uint64)      # 7/4 of 2^64, and 9
+    assert norm_of(several) == (7 * (1 << 62) + 9) % MOD
+    assert ro.clip_factor(MOD - 1, 1 << 32, 16) == 1 << 16
+
+
+def test_the_header_states_the_range():
+    text = header()
+    assert "S is the squared norm only while that is below 2^64, that is, N below 2^32: a real norm below 2^(32-f) at f fractional bits" in text
+    assert "A max_norm of 2^32 or more is never exceeded" in text
+    assert "which it is only while that sum is below 2^64" in text
