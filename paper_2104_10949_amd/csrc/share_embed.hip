@@ -102,11 +102,12 @@ __global__ __launch_bounds__(THREADS) void embed_grad_kernel(const u64* __restri
     }
 }
 
-// ---- gradient with scratch memory: tokens grouped by id, every row of the gradient written once ----
+// ---- gradient with scratch memory: tokens grouped by id ----
 // The sums do not depend on the order, so grouping is all the sorting there has to be: a count per row, a place in one
 // list for each row's tokens (handed out by a cursor, in whatever order), the list.  Then one group of lanes per row and
-// piece adds up the row's tokens and writes the row.  Rows of more than `most` tokens are cut into items of that many, which
-// are added to the row atomically: a frequent token must not keep one wave busy to the end.
+// piece adds up the row's tokens and writes the row, once.  Rows of more than `most` tokens are cut into items of that many, which
+// are added to the row atomically: a frequent token must not keep one wave busy to the end.  Such a row is cleared by a
+// launch before the sums' (or holds what is added to), and so is every row where the whole table is cleared first.
 
 struct Item {
     unsigned row, first, count, whole;   // whole: all of the row's tokens
@@ -143,10 +144,14 @@ const u64 MIDDLING_ROWS = (u64)BUCKETS * 8 * GROUP_THREADS;
 Grouped grouped_layout(char* p, u64 n, u64 V, u64 D) {
     Grouped g = {};
     // a wave takes two microseconds for eight tokens: items short enough for 8192 waves of 256 words, and in a large call
-    // long enough to need few atomics (63904 tokens of 320 x 105: 53 us with 4 tokens, 36 with 8, 29 with 16, 58 with 64)
+    // long enough to need few atomics (63904 tokens of 320 x 105: 53 us with 4 tokens, 36 with 8, 29 with 16, 58 with 64; items of at
+    // least 8 or 16 tokens, the whole call: 2000 tokens of 30000 x 64 14.9 us and 17.1, 4096 of 32000 x 768 86.8 and 87.6, but 4096 of
+    // 1000 x 768 27.8 and 26.7, of 300 x 2048 49.7 and 46.6)
     g.middling = n <= MIDDLING && V <= MIDDLING_ROWS;
     // a row with tokens is then written twice, but its clearing is hidden, and writes go faster without reads among them (4096 tokens of
-    // 32000 x 768: 84 us, 87 with the rows without tokens cleared by the sums' launch; 2000 of 128000 x 255: 96 and 109)
+    // 32000 x 768: 84 us, 87 with the rows without tokens cleared by the sums' launch; 2000 of 128000 x 255: 96 and 109; at the
+    // border 12000 of 32000 x 768 113.1 and 113.4, 17000 132.4 and 131.3, 5000 of 8000 x 2048 94.2 and 92.9).  A table of positions, which
+    // leaves few rows without tokens, would be better off without: 8192 of 8192 x 700 56.9 and 49.8, of 2048 x 700 36.5 and 36.0.
     g.clear_first = g.middling && n * D <= 6000000 + V * D / 5;
     g.buckets = 32;   // (16 to 64 are alike; 128 keep the clearing waiting, 5 us of 68)
     while (g.buckets < BUCKETS && (u64)g.buckets * 8 * GROUP_THREADS < V) g.buckets *= 2;
@@ -581,8 +586,8 @@ void launch_embed(const u64* ta, const u64* tb, const void* ids, u64 alpha, u64*
 // The first blocks hold all ids in LDS, and each of their waves has a token and a share of its row: ballots over the ids name
 // the tokens of the same row, and the first of them adds them all up.  A row with more than OWN tokens waits until the
 // block has come to its end: then the waves share its tokens out and meet in LDS.  The other blocks clear the rows without
-// tokens, which they know from one bit per row in LDS.  (777 tokens of 1531 x 515: 14 us, 19 in two launches by way of a
-// list; clearing and then adding word by word is 16 us there, 15 instead of 12 at 16 to 256 tokens.)
+// tokens, which they know from one bit per row in LDS.  (777 tokens of 1531 x 515: 12.9 us; 14 when this way was chosen, against 19
+// in two launches by way of a list and 16 for clearing and then adding word by word, which is 15 instead of 12 at 16 to 256 tokens.)
 const int FEW = 1024, FEW_THREADS = 512, WAVES = FEW_THREADS / 64;
 const int FEW_ROWS = 1 << 18;
 // Sixteen rows under way at a time and pieces of one access per lane: what counts in these calls is the time of a round trip to

@@ -106,7 +106,8 @@ struct Pairs {
 // A group of 2^lg lanes per head: first the pairs that are turned, UNROLL units per lane under way, then the elements that
 // are only scaled.  Lanes behind the end read the last unit again and write nothing.  A position outside the table has
 // zeros for its angles and for the scale.  Bound by memory (four to eight products of 64 bits per element are a quarter of
-// the vector units' time): 4096 x 25 heads of 128 in 48 us right after the sums, 6.6 TB/s; the gradient of 2048 x 25 in 47 us, 5.6.
+// the vector units' time): 4096 x 25 heads of 128 in 48 us right after the sums, 6.6 TB/s with what those left in the caches; the gradient of
+// 2048 x 25 in 47 us, 5.6.
 template <bool GRAD, int W, bool INTER>
 __global__ __launch_bounds__(THREADS) void rotate_kernel(HeadParams p, int lg) {
     typedef Pairs<W, INTER> P;

@@ -63,7 +63,8 @@ const int NORM_UNROLL = 8;   // loads of each component under way per lane
 // components, 64 MB of the 256 MB that the memory-side cache holds) are therefore read as what is wanted again, and
 // clipping begins at the end; what lies before them streams past the caches, which is faster for the norm.  Norm of 25.5
 // million elements alone, norm and clipping of 19.3 million: 64, 52 and 103 us this way, 68, 52 and 102 with 128 MB kept, 71, 53 and
-// 96 with 192 MB; with plain accesses and clipping from the beginning 82, 87 and 101.
+// 96 with 192 MB; with plain accesses and clipping from the beginning 82, 87 and 101.  (What the norm alone gains from
+// 192 to 64 MB, 7 us, norm and clipping lose, 6: a norm that is only watched has no call after it to win them back.)
 const u64 KEEP_WORDS = (u64)4 << 20;
 
 template <bool KEEP>
