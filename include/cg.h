@@ -635,8 +635,9 @@ CG_API size_t cg_share_embedding_grad_workspace_bytes(size_t n, size_t V, size_t
  *              integers, signed, of pos_bytes = 4 or 8 bytes.  A position outside [0, positions) gives
  *              a row of zeros (z, dx and dr).
  *   interleaved : 0 pairs element p with p + rot/2, 1 pairs 2p with 2p + 1
- *   rot      : even, 0 <= rot <= dim; 0 turns nothing, and cos, sin, pos may be NULL (a three-term
- *              product with one shared word per head, e.g. the last step of the norm's gradient)
+ *   rot      : even, 0 <= rot <= dim; 0 turns nothing and reads no position: every row counts, and cos,
+ *              sin, pos may be NULL (a three-term product with one shared word per head, e.g. the
+ *              last step of the norm's gradient)
  *   ld_g, ld_out : words from a row to the next of g, and of z or dx (>= heads*dim; what lies
  *              between the rows is left alone).  r, dr and the sums are contiguous.
  *

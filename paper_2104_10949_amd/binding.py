@@ -793,7 +793,7 @@ def cg_share_head_norm_rotate(x_i, x_ip1, r_i, r_ip1, cos=None, sin=None, pos=No
                               z_i=None, stream=None) -> torch.Tensor:
     """z_i [rows, heads, dim]: three-term product of each head with its shared inverse norm r [rows, heads], the first
     rot = 2 * cos.shape[1] elements turned by the public angles of the row's position, the others times 2^frac_bits.  Without
-    angles the product alone, times 2^frac_bits."""
+    angles, or with angles of no pairs, the product alone, times 2^frac_bits: no position is read, and no row is zero for its own."""
     shape = x_i.shape
     ld_x = _pair_step(x_i, x_ip1, shape)
     if z_i is None:

@@ -1,4 +1,4 @@
-"""The calls over heads on pairs whose components lie in memory in different ways that come to the same row step, against the
+"""The calls over heads without a turn, and on pairs whose components lie in memory in different ways that come to the same row step, against the
 oracle, bit for bit."""
 import numpy as np
 import pytest
@@ -45,3 +45,18 @@ def test_components_that_lie_differently(rows, count, dim, first, second):
     want = (ro.head_sq_sum(*x), ro.head_norm_rotate(*x, *r, **kw), *ro.head_norm_rotate_grad(*g, *x, *r, **kw))
     for a, w in zip(got, want):
         assert np.array_equal(cg.to_host(a), w)
+
+
+def test_angles_of_no_pairs_read_no_position():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from oracle import ring_oracle as ro
+    from paper_2104_10949_amd import binding as cg, workloads as wl
+    say("heads with angles of no pairs")
+    x, r = [wl.draw_ring((4, 2, 6), 510 + k) for k in range(2)], [wl.draw_ring((4, 2), 512 + k) for k in range(2)]
+    none, pos = torch.empty((9, 0), dtype=torch.int64, device="cuda"), torch.tensor([0, -1, 9, 3], device="cuda")
+    dx, dr = [cg.to_device(a) for a in x], [cg.to_device(a) for a in r]
+    z = cg.cg_share_head_norm_rotate(*dx, *dr, none, none, pos, frac_bits=5)
+    assert np.array_equal(cg.to_host(z), ro.head_norm_rotate(*x, *r, frac_bits=5))
+    for got, want in zip(cg.cg_share_head_norm_rotate_grad(*dx, *dx, *dr, none, none, pos, frac_bits=5), ro.head_norm_rotate_grad(*x, *x, *r, frac_bits=5)):
+        assert np.array_equal(cg.to_host(got), want)
